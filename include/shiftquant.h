@@ -665,6 +665,154 @@ sq_status sq_l1bn_backward(const float* dy, int64_t M, int64_t C, int64_t ld_dy,
                            float* dgamma, float* dbeta, uint8_t* group, sq_scale* gscale,
                            uint32_t* dx_ranges, void* workspace, size_t workspace_bytes, void* stream);
 
+/* ===========================================================================
+ * Microscaled 4-bit linear layers.
+ *
+ * The same three products as the integer path, Y = X W^T, dX = dY W and
+ * dW = dY^T X, with operands in microscaled 4-bit floating point (E2M1
+ * elements, one E8M0 scale for 32 consecutive elements of a product's inner
+ * axis) and fp32 accumulation on the matrix cores, dense or by expert.
+ *
+ * A block of 32 with largest magnitude a:
+ *   s    = the smallest byte with a / 2^(s - 127) <= 7 (at least 0)
+ *   code = x / 2^(s - 127) rounded to the nearest of +-{0, 0.5, 1, 1.5, 2, 3,
+ *          4, 6}, ties to the even code (so no element is off by more than half
+ *          a step: 7 is halfway from 6 to the next power of two);
+ *   a block that holds NaN or Inf: s = 255, which stands for NaN in all of it.
+ * Every value that a code and scale stand for is exact in bf16 and fp32, but
+ * 4 * 2^126 (of a block with a > 1.75 * 2^127), which is past their range: Inf.
+ *
+ * Layout of a matrix [rows, K] (sq_mx_size bytes): rows in groups of 16, K in
+ * units of 512.  Element (r, k) is nibble k % 2 (0: low) of byte
+ *   ((r / 16) * units + k / 512) * 4096 + (k / 128) % 4 * 1024
+ *       + (k / 32) % 4 * 256 + (r % 16) * 16 + (k % 32) / 2,
+ * its block's scale byte
+ *   ((r / 16) * units + k / 512) * 256 + (k / 32) % 4 * 64 + (r % 16) * 4 + (k / 128) % 4.
+ * This is the operand order of v_mfma_scale_f32_16x16x128_f8f6f4: a wave
+ * loads a 16 x 128 tile as one contiguous 1 KB block.  Writers fill K up to the
+ * next multiple of 128 with zeros; the rest of the padding is not written
+ * and never used.  Matrices of a stack follow each other without a gap.
+ * codes must be 16-byte aligned, scales 4-byte.
+ *
+ * By expert: `offsets` [experts + 1] (device memory) splits the rows; expert
+ * e owns [offsets[e], offsets[e + 1]), possibly none.  Offsets ascend from
+ * >= 0 to <= rows; rows outside of them are neither read nor written.
+ * Offsets that break this never lead out of the buffers, but what is
+ * computed is then unspecified.  The inner axis of the transposed form
+ * starts anew at a multiple of 512 for each expert: expert e's rows are
+ * columns P_e + (row - offsets[e]), P_e = sum over e' < e of
+ * roundup(rows of e', 512), of a matrix with sq_mx_segment_cols columns.
+ * ========================================================================= */
+
+/* Element types of the arguments named `type`. */
+enum {
+    SQ_TYPE_F32 = 0,
+    SQ_TYPE_BF16 = 1
+};
+
+sq_status sq_mx_size(int64_t rows, int64_t cols, size_t* code_bytes, size_t* scale_bytes);
+sq_status sq_mx_segment_cols(int64_t rows, int64_t experts, int64_t* cols);
+
+/* ---------------------------------------------------------------------------
+ * sq_mx_quantize -- codes of X [batch, rows, cols] (row stride ld, matrix stride
+ * `stride`, both in elements) in one read, along either axis or both:
+ *   codes, scales      [batch] matrices [rows, cols], blocks along the columns
+ *                      (the operand of a product over the columns)
+ *   codes_t, scales_t  [batch] matrices [cols, rows], blocks along the rows (of a
+ *                      product over the rows)
+ * Either pair may be NULL, not both.  With offsets (batch == 1): codes_t is
+ * [cols, sq_mx_segment_cols(rows, experts)], its blocks start anew at each
+ * expert's first row.
+ * Errors: SQ_ERR_INVALID_ARGUMENT, SQ_ERR_UNSUPPORTED (rows >= 2^23 with
+ * codes_t), SQ_ERR_HIP.
+ * ------------------------------------------------------------------------- */
+sq_status sq_mx_quantize(const void* X, int32_t type, int64_t batch, int64_t rows, int64_t cols, int64_t ld, int64_t stride,
+                         const int32_t* offsets, int64_t experts,
+                         uint8_t* codes, uint8_t* scales, uint8_t* codes_t, uint8_t* scales_t, void* stream);
+
+/* sq_mx_dequantize -- the values [rows, cols] of a matrix, as fp32 or bf16 (exact in both). */
+sq_status sq_mx_dequantize(const uint8_t* codes, const uint8_t* scales, int64_t rows, int64_t cols,
+                           void* out, int32_t type, int64_t ld, void* stream);
+
+/* ---------------------------------------------------------------------------
+ * sq_mx_gemm -- C [M, N] = A B^T, A [M, K], B [N, K]; C fp32, or bf16 rounded
+ * once to the nearest even.  K = 0 gives zeros.
+ * Workspace: sq_mx_gemm_workspace_size bytes (0: none), 16-byte aligned.
+ * Errors: SQ_ERR_INVALID_ARGUMENT, SQ_ERR_UNSUPPORTED (K >= 2^23),
+ * SQ_ERR_WORKSPACE_TOO_SMALL, SQ_ERR_HIP.
+ * ------------------------------------------------------------------------- */
+sq_status sq_mx_gemm_workspace_size(int64_t M, int64_t N, int64_t K, size_t* bytes);
+sq_status sq_mx_gemm(const uint8_t* A, const uint8_t* A_scales, const uint8_t* B, const uint8_t* B_scales,
+                     int64_t M, int64_t N, int64_t K, void* C, int32_t type, int64_t ldc,
+                     void* workspace, size_t workspace_bytes, void* stream);
+
+/* ---------------------------------------------------------------------------
+ * sq_mx_gemm_experts -- C[m] = A[m] B_e^T for the rows m of each expert e:
+ * A [M, K], B a stack [experts] of [N, K], C [M, N].  The forward pass with W
+ * stacks, the input gradient with W^T stacks.  Errors as sq_mx_gemm.
+ * ------------------------------------------------------------------------- */
+sq_status sq_mx_gemm_experts(const uint8_t* A, const uint8_t* A_scales, int64_t M, int64_t K,
+                             const int32_t* offsets, int64_t experts,
+                             const uint8_t* B, const uint8_t* B_scales, int64_t N,
+                             void* C, int32_t type, int64_t ldc, void* stream);
+
+/* ---------------------------------------------------------------------------
+ * sq_mx_gemm_experts_wgrad -- C_e [M, N] = sum over the rows r of expert e of
+ * A[:, r] B[:, r]^T: A [M, sq_mx_segment_cols(rows, experts)] and B [N, same]
+ * are the transposed forms that sq_mx_quantize wrote with the same offsets;
+ * C is a stack [experts] of [M, ldc].  An expert without rows gets zeros.
+ * Workspace: sq_mx_gemm_experts_wgrad_workspace_size bytes (0: none).
+ * Errors: as sq_mx_gemm; SQ_ERR_UNSUPPORTED for rows >= 2^23.
+ * ------------------------------------------------------------------------- */
+sq_status sq_mx_gemm_experts_wgrad_workspace_size(int64_t rows, int64_t experts, int64_t M, int64_t N, size_t* bytes);
+sq_status sq_mx_gemm_experts_wgrad(const uint8_t* A, const uint8_t* A_scales, const uint8_t* B, const uint8_t* B_scales,
+                                   int64_t rows, const int32_t* offsets, int64_t experts, int64_t M, int64_t N,
+                                   void* C, int32_t type, int64_t ldc,
+                                   void* workspace, size_t workspace_bytes, void* stream);
+
+/* ---------------------------------------------------------------------------
+ * sq_mx_linear -- Y [M, N] = X W^T with X [M, K] in fp32 or bf16, quantized on the
+ * way: what sq_mx_quantize and sq_mx_gemm (offsets NULL, experts 0) or
+ * sq_mx_gemm_experts give.  Few rows (at most 16, or 16 an expert on average)
+ * take one launch and no workspace, the serving form for single tokens.
+ * Workspace: sq_mx_linear_workspace_size bytes (0: none), 16-byte aligned.
+ * Errors: as sq_mx_gemm.
+ * ------------------------------------------------------------------------- */
+sq_status sq_mx_linear_workspace_size(int64_t M, int64_t K, int64_t N, int64_t experts, size_t* bytes);
+sq_status sq_mx_linear(const void* X, int32_t type, int64_t M, int64_t K, int64_t ld,
+                       const int32_t* offsets, int64_t experts,
+                       const uint8_t* W, const uint8_t* W_scales, int64_t N,
+                       void* Y, int32_t out_type, int64_t ldy,
+                       void* workspace, size_t workspace_bytes, void* stream);
+
+/* ---------------------------------------------------------------------------
+ * sq_act_forward, sq_act_backward -- an activation between two layers, whose
+ * backward pass reads a copy of its input in 8 bits.
+ *   SQ_ACT_SILU  act(x) = x sigma(x)
+ *   SQ_ACT_GELU  act(x) = x sigma(2 sqrt(2 / pi) (x + 0.044715 x^3)), the tanh form
+ * gated == 0: X [M, F],   H = act(X),      dX = dH act'(x)
+ * gated == 1: X [M, 2 F], the gate g first, H = act(g) u,
+ *             dX = (dH u act'(g), dH act(g))
+ * The forward is computed from X, the backward from the copy: x stands as
+ * code 2^(s - 127), code an int8 in [-127, 127], s one byte for 32 consecutive
+ * columns of g or of u, the smallest with max |x| / 2^(s - 127) < 127.5 (255, for
+ * NaN in the whole block, where it holds NaN or Inf).  codes [M, n Fp] with
+ * Fp = roundup(F, 32) and n = 1 or 2, g in columns [0, F), u in [Fp, Fp + F);
+ * scales [M, n Fp / 32]; sizes from sq_act_size.  codes must be 16-byte
+ * aligned.  X, H, dH and dX share one type; sums in fp32, rounded once.
+ * Errors: SQ_ERR_INVALID_ARGUMENT, SQ_ERR_UNSUPPORTED, SQ_ERR_HIP.
+ * ------------------------------------------------------------------------- */
+enum {
+    SQ_ACT_SILU = 0,
+    SQ_ACT_GELU = 1
+};
+
+sq_status sq_act_size(int64_t M, int64_t F, int32_t gated, size_t* code_bytes, size_t* scale_bytes);
+sq_status sq_act_forward(const void* X, int32_t type, int32_t kind, int32_t gated, int64_t M, int64_t F, int64_t ld_x,
+                         void* H, int64_t ld_h, int8_t* codes, uint8_t* scales, void* stream);
+sq_status sq_act_backward(const void* dH, int32_t type, int32_t kind, int32_t gated, int64_t M, int64_t F, int64_t ld_h,
+                          const int8_t* codes, const uint8_t* scales, void* dX, int64_t ld_x, void* stream);
+
 /* Static description of a status code. */
 const char* sq_status_string(sq_status s);
 

@@ -38,14 +38,11 @@ int64_t fold_ext_max(int64_t C, const QuantCfg& c) {
 
 }  // namespace sq
 
+namespace sq {
+
 namespace {
-
-using namespace sq;
-
 thread_local std::string g_last_error;
-
-constexpr int64_t kMaxRows = (int64_t)1 << 31;      // rows of any operand
-constexpr int64_t kMaxChannels = (int64_t)1 << 20;  // C_out, C_in, cols
+}
 
 sq_status fail(sq_status s, const std::string& msg) {
     g_last_error = msg;
@@ -56,6 +53,15 @@ sq_status hip_status(hipError_t e, const char* what) {
     if (e == hipSuccess) return SQ_OK;
     return fail(SQ_ERR_HIP, std::string(what) + ": " + hipGetErrorString(e));
 }
+
+}  // namespace sq
+
+namespace {
+
+using namespace sq;
+
+constexpr int64_t kMaxRows = (int64_t)1 << 31;      // rows of any operand
+constexpr int64_t kMaxChannels = (int64_t)1 << 20;  // C_out, C_in, cols
 
 bool aligned(const void* p, uintptr_t a) { return (reinterpret_cast<uintptr_t>(p) % a) == 0; }
 

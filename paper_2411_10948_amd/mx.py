@@ -1,0 +1,340 @@
+"""Microscaled 4-bit linear layers, dense or by expert, and activations whose
+backward pass reads an 8-bit copy of their input (include/shiftquant.h has the
+formats, formulas and layouts).
+
+As in the ``shiftquant`` module, the functions named ``sq_*`` marshal torch
+tensors to the C entry points one to one, and the layer above them keeps the
+buffers: ``LinearPlan`` and ``ActPlan`` allocate everything a layer needs once,
+for a fixed shape, and their calls only enqueue work.
+"""
+from __future__ import annotations
+
+import ctypes as ct
+import dataclasses
+from typing import Optional, Tuple
+
+import torch
+
+from .shiftquant import _I64, _SZ, _check, _ptr, _stream, _ws_ptr, load
+
+TYPE_F32 = 0
+TYPE_BF16 = 1
+ACT_SILU = 0
+ACT_GELU = 1
+ACT_KINDS = {"silu": ACT_SILU, "gelu": ACT_GELU}
+
+_TYPES = {torch.float32: TYPE_F32, torch.bfloat16: TYPE_BF16}
+
+
+def _type(t: torch.Tensor) -> int:
+    """SQ_TYPE_* of a tensor of values on the GPU."""
+    if not t.is_cuda:
+        raise ValueError("expected a tensor on the GPU")
+    try:
+        return _TYPES[t.dtype]
+    except KeyError:
+        raise TypeError(f"expected float32 or bfloat16, got {t.dtype}") from None
+
+
+def _rows(t: torch.Tensor, name: str) -> int:
+    """Row stride of a 2-D tensor with unit column stride."""
+    st = t.stride()
+    if len(st) != 2 or (st[1] != 1 and t.shape[1] > 1):
+        raise ValueError(f"{name}: expected a 2-D tensor with unit column stride")
+    return st[0] if t.shape[0] > 1 else max(st[0], t.shape[1])
+
+
+def _shape(t: torch.Tensor, shape, name: str) -> None:
+    if tuple(t.shape) != tuple(shape):
+        raise ValueError(f"{name}: expected shape {tuple(shape)}, got {tuple(t.shape)}")
+
+
+def _offsets(offsets: Optional[torch.Tensor], experts: int) -> Optional[int]:
+    if offsets is None:
+        if experts:
+            raise ValueError("offsets: missing")
+        return None
+    if (offsets.dtype != torch.int32 or offsets.shape != (experts + 1,) or not offsets.is_contiguous()
+            or not offsets.is_cuda):
+        raise ValueError(f"offsets: expected {experts + 1} contiguous int32 values on the GPU")
+    return offsets.data_ptr()
+
+
+@dataclasses.dataclass
+class MxMatrix:
+    """A matrix [rows, cols] in microscaled 4-bit codes, or a stack of them
+    (codes and scales are then [stack, bytes of a matrix])."""
+    codes: torch.Tensor
+    scales: torch.Tensor
+    rows: int
+    cols: int
+    stack: int = 0      # 0: one matrix, or as many as codes has rows
+
+    def __post_init__(self):
+        nc, ns = sq_mx_size(self.rows, self.cols)
+        if self.stack == 0 and self.codes.dim() == 2 and self.codes.shape[0] > 1:
+            self.stack = self.codes.shape[0]
+        n = max(self.stack, 1)
+        for t, size, name in ((self.codes, nc, "codes"), (self.scales, ns, "scales")):
+            if t.dtype != torch.uint8 or not t.is_contiguous() or t.numel() < n * size:
+                raise ValueError(f"{name}: expected at least {n * size} contiguous uint8 values")
+
+    @classmethod
+    def empty(cls, rows: int, cols: int, stack: int = 0, device="cuda") -> "MxMatrix":
+        nc, ns = sq_mx_size(rows, cols)
+        n = max(stack, 1)
+        return cls(torch.empty((n, nc), dtype=torch.uint8, device=device),
+                   torch.empty((n, ns), dtype=torch.uint8, device=device), rows, cols, stack)
+
+    def values(self, dtype=torch.float32, stream=None) -> torch.Tensor:
+        """The values that the codes stand for (exact in float32 and bfloat16)."""
+        nc, ns = sq_mx_size(self.rows, self.cols)
+        out = torch.empty((max(self.stack, 1), self.rows, self.cols), dtype=dtype, device=self.codes.device)
+        codes, scales = self.codes.view(-1), self.scales.view(-1)
+        for i in range(out.shape[0]):
+            sq_mx_dequantize(codes[i * nc:], scales[i * ns:], self.rows, self.cols, out[i], stream)
+        return out if self.stack else out[0]
+
+
+# ---------------------------------------------------------------------------
+# one-to-one wrappers of the C entry points
+# ---------------------------------------------------------------------------
+def sq_mx_size(rows: int, cols: int) -> Tuple[int, int]:
+    """(bytes of the codes, bytes of the scales)"""
+    a, b = _SZ(0), _SZ(0)
+    _check("sq_mx_size", load().sq_mx_size(rows, cols, ct.byref(a), ct.byref(b)))
+    return a.value, b.value
+
+
+def sq_mx_segment_cols(rows: int, experts: int) -> int:
+    n = _I64(0)
+    _check("sq_mx_segment_cols", load().sq_mx_segment_cols(rows, experts, ct.byref(n)))
+    return n.value
+
+
+def sq_mx_quantize(X, codes, scales, codes_t, scales_t, offsets=None, experts=0, stream=None) -> None:
+    """X [rows, cols] or [batch, rows, cols]"""
+    if X.dim() == 3:
+        batch, (rows, cols) = X.shape[0], X.shape[1:]
+        if cols > 1 and X.stride(2) != 1:
+            raise ValueError("X: expected unit column stride")
+        ld, stride = (X.stride(1) if rows > 1 else max(X.stride(1), cols)), X.stride(0)
+    else:
+        (rows, cols), batch, ld, stride = X.shape, 1, _rows(X, "X"), 0
+    _check("sq_mx_quantize", load().sq_mx_quantize(
+        _ptr(X), _type(X), batch, rows, cols, ld, stride, _offsets(offsets, experts), experts, _ptr(codes), _ptr(scales),
+        _ptr(codes_t), _ptr(scales_t), _stream(stream)))
+
+
+def sq_mx_dequantize(codes, scales, rows, cols, out, stream=None) -> None:
+    _shape(out, (rows, cols), "out")
+    _check("sq_mx_dequantize", load().sq_mx_dequantize(
+        _ptr(codes), _ptr(scales), rows, cols, _ptr(out), _type(out), _rows(out, "out"), _stream(stream)))
+
+
+def sq_mx_gemm_workspace_size(M: int, N: int, K: int) -> int:
+    nb = _SZ(0)
+    _check("sq_mx_gemm_workspace_size", load().sq_mx_gemm_workspace_size(M, N, K, ct.byref(nb)))
+    return nb.value
+
+
+def sq_mx_gemm(A, A_scales, B, B_scales, K, C, workspace=None, stream=None) -> None:
+    M, N = C.shape
+    ws, nws = _ws_ptr(workspace)
+    _check("sq_mx_gemm", load().sq_mx_gemm(
+        _ptr(A), _ptr(A_scales), _ptr(B), _ptr(B_scales), M, N, K, _ptr(C), _type(C), _rows(C, "C"), ws, nws,
+        _stream(stream)))
+
+
+def sq_mx_gemm_experts(A, A_scales, K, offsets, experts, B, B_scales, C, stream=None) -> None:
+    M, N = C.shape
+    _check("sq_mx_gemm_experts", load().sq_mx_gemm_experts(
+        _ptr(A), _ptr(A_scales), M, K, _offsets(offsets, experts), experts, _ptr(B), _ptr(B_scales), N, _ptr(C), _type(C),
+        _rows(C, "C"), _stream(stream)))
+
+
+def sq_mx_gemm_experts_wgrad_workspace_size(rows: int, experts: int, M: int, N: int) -> int:
+    nb = _SZ(0)
+    _check("sq_mx_gemm_experts_wgrad_workspace_size",
+           load().sq_mx_gemm_experts_wgrad_workspace_size(rows, experts, M, N, ct.byref(nb)))
+    return nb.value
+
+
+def sq_mx_gemm_experts_wgrad(A, A_scales, B, B_scales, rows, offsets, experts, C, workspace=None, stream=None) -> None:
+    """C [experts, M, N], contiguous"""
+    if C.dim() != 3 or C.shape[0] != experts or not C.is_contiguous():
+        raise ValueError("C: expected a contiguous [experts, M, N] tensor")
+    ws, nws = _ws_ptr(workspace)
+    _check("sq_mx_gemm_experts_wgrad", load().sq_mx_gemm_experts_wgrad(
+        _ptr(A), _ptr(A_scales), _ptr(B), _ptr(B_scales), rows, _offsets(offsets, experts), experts, C.shape[1], C.shape[2],
+        _ptr(C), _type(C), max(C.shape[2], 1), ws, nws, _stream(stream)))
+
+
+def sq_mx_linear_workspace_size(M: int, K: int, N: int, experts: int = 0) -> int:
+    nb = _SZ(0)
+    _check("sq_mx_linear_workspace_size", load().sq_mx_linear_workspace_size(M, K, N, experts, ct.byref(nb)))
+    return nb.value
+
+
+def sq_mx_linear(X, W, W_scales, Y, workspace=None, offsets=None, experts=0, stream=None) -> None:
+    M, K = X.shape
+    N = Y.shape[1]
+    ws, nws = _ws_ptr(workspace)
+    _check("sq_mx_linear", load().sq_mx_linear(
+        _ptr(X), _type(X), M, K, _rows(X, "X"), _offsets(offsets, experts), experts, _ptr(W), _ptr(W_scales), N, _ptr(Y),
+        _type(Y), _rows(Y, "Y"), ws, nws, _stream(stream)))
+
+
+def sq_act_size(M: int, F: int, gated: bool) -> Tuple[int, int]:
+    a, b = _SZ(0), _SZ(0)
+    _check("sq_act_size", load().sq_act_size(M, F, int(gated), ct.byref(a), ct.byref(b)))
+    return a.value, b.value
+
+
+def sq_act_forward(X, kind, gated, H, codes, scales, stream=None) -> None:
+    M, F = H.shape
+    _check("sq_act_forward", load().sq_act_forward(
+        _ptr(X), _type(X), kind, int(gated), M, F, _rows(X, "X"), _ptr(H), _rows(H, "H"), _ptr(codes), _ptr(scales),
+        _stream(stream)))
+
+
+def sq_act_backward(dH, kind, gated, codes, scales, dX, stream=None) -> None:
+    M, F = dH.shape
+    _check("sq_act_backward", load().sq_act_backward(
+        _ptr(dH), _type(dH), kind, int(gated), M, F, _rows(dH, "dH"), _ptr(codes), _ptr(scales), _ptr(dX), _rows(dX, "dX"),
+        _stream(stream)))
+
+
+# ---------------------------------------------------------------------------
+# layers
+# ---------------------------------------------------------------------------
+def _workspace(nbytes: int, device) -> Optional[torch.Tensor]:
+    return torch.empty(nbytes, dtype=torch.uint8, device=device) if nbytes else None
+
+
+def quantize(X: torch.Tensor, rows: bool = True, cols: bool = False, offsets: Optional[torch.Tensor] = None,
+             stream=None) -> Tuple[Optional[MxMatrix], Optional[MxMatrix]]:
+    """Codes of X [rows, cols] (or a stack of such) with blocks along its columns
+    (``rows``: the operand X) and along its rows (``cols``: the operand X^T, by
+    expert with ``offsets``), in one read."""
+    stack = X.shape[0] if X.dim() == 3 else 0
+    M, C = X.shape[-2:]
+    experts = 0 if offsets is None else offsets.shape[0] - 1
+    a = MxMatrix.empty(M, C, stack, X.device) if rows else None
+    t = MxMatrix.empty(C, sq_mx_segment_cols(M, experts) if experts else M, stack, X.device) if cols else None
+    sq_mx_quantize(X, a and a.codes, a and a.scales, t and t.codes, t and t.scales, offsets, experts, stream)
+    return a, t
+
+
+class LinearPlan:
+    """A linear layer Y = X W^T on M rows with microscaled 4-bit operands, all of
+    its buffers allocated once.  ``experts`` > 0: that many weight matrices; the
+    rows are sorted by expert and ``offsets`` [experts + 1] says where each
+    expert's begin (any split of the M rows).
+
+    Serving: ``forward(x, w)`` with W's codes.  Training (``train=True``):
+    ``quantize_weight(W)``, ``forward(x)``, then ``backward(dy)``, which gives dX in
+    the layer's type and dW in float32; the forward keeps X's codes and the
+    offsets for it.  Results are the plan's buffers, overwritten by its next
+    call of the same kind."""
+
+    def __init__(self, M: int, C_in: int, C_out: int, dtype=torch.bfloat16, experts: int = 0, train: bool = False,
+                 device="cuda"):
+        if dtype not in _TYPES:
+            raise TypeError(f"dtype: expected float32 or bfloat16, got {dtype}")
+        dev = torch.device(device)
+        self.M, self.C_in, self.C_out, self.dtype, self.experts, self.train = M, C_in, C_out, dtype, experts, train
+        self.Y = torch.empty((M, C_out), dtype=dtype, device=dev)
+        self.offsets = None
+        if not train:
+            self.ws = _workspace(sq_mx_linear_workspace_size(M, C_in, C_out, experts), dev)
+            return
+        inner = sq_mx_segment_cols(M, experts) if experts else M
+        self.w = MxMatrix.empty(C_out, C_in, experts, dev)
+        self.w_t = MxMatrix.empty(C_in, C_out, experts, dev)
+        self.x, self.x_t = MxMatrix.empty(M, C_in, 0, dev), MxMatrix.empty(C_in, inner, 0, dev)
+        self.dy, self.dy_t = MxMatrix.empty(M, C_out, 0, dev), MxMatrix.empty(C_out, inner, 0, dev)
+        self.dX = torch.empty((M, C_in), dtype=dtype, device=dev)
+        self.dW = torch.empty((experts, C_out, C_in) if experts else (C_out, C_in), dtype=torch.float32, device=dev)
+        if experts:
+            need = sq_mx_gemm_experts_wgrad_workspace_size(M, experts, C_out, C_in)
+        else:
+            need = max(sq_mx_gemm_workspace_size(M, C_out, C_in), sq_mx_gemm_workspace_size(M, C_in, C_out),
+                       sq_mx_gemm_workspace_size(C_out, C_in, M))
+        self.ws = _workspace(need, dev)
+
+    def quantize_weight(self, W: torch.Tensor, stream=None) -> None:
+        """W [C_out, C_in], or [experts, C_out, C_in]"""
+        _shape(W, (self.experts, self.C_out, self.C_in) if self.experts else (self.C_out, self.C_in), "W")
+        sq_mx_quantize(W, self.w.codes, self.w.scales, self.w_t.codes, self.w_t.scales, stream=stream)
+
+    def forward(self, x: torch.Tensor, w: Optional[MxMatrix] = None, offsets: Optional[torch.Tensor] = None, stream=None):
+        _shape(x, (self.M, self.C_in), "x")
+        if not self.train:
+            if w is None or (w.rows, w.cols, max(w.stack, 1)) != (self.C_out, self.C_in, max(self.experts, 1)):
+                raise ValueError(f"w: expected codes of {self.experts or 'one'} [{self.C_out}, {self.C_in}]")
+            if w.codes.device != x.device:
+                raise ValueError("w: expected codes on the device of x")
+            sq_mx_linear(x, w.codes, w.scales, self.Y, self.ws, offsets, self.experts, stream)
+            return self.Y
+        if w is not None:
+            raise ValueError("w: a training plan has its own codes (quantize_weight)")
+        self.offsets = offsets
+        sq_mx_quantize(x, self.x.codes, self.x.scales, self.x_t.codes, self.x_t.scales, offsets, self.experts, stream)
+        self._product(self.x, self.w, self.C_in, self.Y, stream)
+        return self.Y
+
+    def _product(self, a: MxMatrix, b: MxMatrix, K: int, C: torch.Tensor, stream) -> None:
+        if self.experts:
+            sq_mx_gemm_experts(a.codes, a.scales, K, self.offsets, self.experts, b.codes, b.scales, C, stream)
+        else:
+            sq_mx_gemm(a.codes, a.scales, b.codes, b.scales, K, C, self.ws, stream)
+
+    def backward(self, dy: torch.Tensor, stream=None):
+        """(dX, dW) of the last forward"""
+        if not self.train:
+            raise ValueError("backward needs a plan with train=True")
+        _shape(dy, (self.M, self.C_out), "dy")
+        sq_mx_quantize(dy, self.dy.codes, self.dy.scales, self.dy_t.codes, self.dy_t.scales, self.offsets, self.experts,
+                       stream)
+        self._product(self.dy, self.w_t, self.C_out, self.dX, stream)
+        if self.experts:
+            sq_mx_gemm_experts_wgrad(self.dy_t.codes, self.dy_t.scales, self.x_t.codes, self.x_t.scales, self.M,
+                                     self.offsets, self.experts, self.dW, self.ws, stream)
+        else:
+            sq_mx_gemm(self.dy_t.codes, self.dy_t.scales, self.x_t.codes, self.x_t.scales, self.M, self.dW, self.ws, stream)
+        return self.dX, self.dW
+
+
+class ActPlan:
+    """An activation on M rows of F outputs, ``act`` "silu" or "gelu" (tanh form),
+    ``gated``: h = act(g) u of an input [M, 2 F] with the gate first.  The forward
+    keeps the input in 8 bits, the backward reads only that and dh."""
+
+    def __init__(self, M: int, F: int, act: str = "silu", gated: bool = True, dtype=torch.bfloat16, device="cuda"):
+        if act not in ACT_KINDS:
+            raise ValueError(f"act: expected one of {sorted(ACT_KINDS)}, got {act!r}")
+        if dtype not in _TYPES:
+            raise TypeError(f"dtype: expected float32 or bfloat16, got {dtype}")
+        dev = torch.device(device)
+        self.M, self.F, self.kind, self.gated, self.dtype = M, F, ACT_KINDS[act], gated, dtype
+        self.width = 2 * F if gated else F
+        nc, ns = sq_act_size(M, F, gated)
+        self.codes = torch.empty(nc, dtype=torch.int8, device=dev)
+        self.scales = torch.empty(ns, dtype=torch.uint8, device=dev)
+        self.H = torch.empty((M, F), dtype=dtype, device=dev)
+        self.dX = torch.empty((M, self.width), dtype=dtype, device=dev)
+
+    def forward(self, x: torch.Tensor, stream=None) -> torch.Tensor:
+        _shape(x, (self.M, self.width), "x")
+        if x.dtype != self.dtype:
+            raise TypeError(f"x: expected {self.dtype}, got {x.dtype}")
+        sq_act_forward(x, self.kind, self.gated, self.H, self.codes, self.scales, stream)
+        return self.H
+
+    def backward(self, dh: torch.Tensor, stream=None) -> torch.Tensor:
+        _shape(dh, (self.M, self.F), "dh")
+        if dh.dtype != self.dtype:
+            raise TypeError(f"dh: expected {self.dtype}, got {dh.dtype}")
+        sq_act_backward(dh, self.kind, self.gated, self.codes, self.scales, self.dX, stream)
+        return self.dX

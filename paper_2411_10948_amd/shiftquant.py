@@ -48,6 +48,9 @@ EXPORTS = (
     "sq_quantize_grad_conv",
     "sq_conv_wgrad_workspace_size", "sq_conv_wgrad", "sq_gemm_dgrad_range_slabs", "sq_gemm_dgrad_ranged",
     "sq_quantize_grad_noalloc", "sq_conv_dgrad_ranged", "sq_quantize_grad_conv_from_ranges",
+    "sq_mx_size", "sq_mx_segment_cols", "sq_mx_quantize", "sq_mx_dequantize", "sq_mx_gemm_workspace_size", "sq_mx_gemm",
+    "sq_mx_gemm_experts", "sq_mx_gemm_experts_wgrad_workspace_size", "sq_mx_gemm_experts_wgrad",
+    "sq_mx_linear_workspace_size", "sq_mx_linear", "sq_act_size", "sq_act_forward", "sq_act_backward",
     "sq_status_string", "sq_last_error", "sq_last_error_string",
 )
 
@@ -165,6 +168,23 @@ def load() -> ct.CDLL:
         "sq_l1bn_backward": [_P, _I64, _I64, _I64, pp, _P, _I64, _P, _P, _P, _I64, _P, _P, _P, _P, _P, _P, _SZ,
                              _P],
     }
+    i32 = ct.c_int32
+    sig.update({   # wrapped in the mx module
+        "sq_mx_size": [_I64, _I64, ct.POINTER(_SZ), ct.POINTER(_SZ)],
+        "sq_mx_segment_cols": [_I64, _I64, ct.POINTER(_I64)],
+        "sq_mx_quantize": [_P, i32, _I64, _I64, _I64, _I64, _I64, _P, _I64, _P, _P, _P, _P, _P],
+        "sq_mx_dequantize": [_P, _P, _I64, _I64, _P, i32, _I64, _P],
+        "sq_mx_gemm_workspace_size": [_I64, _I64, _I64, ct.POINTER(_SZ)],
+        "sq_mx_gemm": [_P, _P, _P, _P, _I64, _I64, _I64, _P, i32, _I64, _P, _SZ, _P],
+        "sq_mx_gemm_experts": [_P, _P, _I64, _I64, _P, _I64, _P, _P, _I64, _P, i32, _I64, _P],
+        "sq_mx_gemm_experts_wgrad_workspace_size": [_I64, _I64, _I64, _I64, ct.POINTER(_SZ)],
+        "sq_mx_gemm_experts_wgrad": [_P, _P, _P, _P, _I64, _P, _I64, _I64, _I64, _P, i32, _I64, _P, _SZ, _P],
+        "sq_mx_linear_workspace_size": [_I64, _I64, _I64, _I64, ct.POINTER(_SZ)],
+        "sq_mx_linear": [_P, i32, _I64, _I64, _I64, _P, _I64, _P, _P, _I64, _P, i32, _I64, _P, _SZ, _P],
+        "sq_act_size": [_I64, _I64, i32, ct.POINTER(_SZ), ct.POINTER(_SZ)],
+        "sq_act_forward": [_P, i32, i32, i32, _I64, _I64, _I64, _P, _I64, _P, _P, _P],
+        "sq_act_backward": [_P, i32, i32, i32, _I64, _I64, _I64, _P, _P, _P, _I64, _P],
+    })
     for name, args in sig.items():
         f = getattr(L, name)
         f.argtypes = args

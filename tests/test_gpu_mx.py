@@ -1,0 +1,456 @@
+"""Microscaled 4-bit linear layers on the GPU against the plain implementation in
+64 bits (tests/mx_reference.py): codes and scales byte for byte in their
+documented places, products within the bound of an fp32 sum, ragged and empty
+experts, strided and misaligned inputs, NaN, other streams, graph replays."""
+import numpy as np
+import pytest
+
+from tests import mx_reference as ref
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def mx():
+    import torch
+    assert torch.cuda.is_available(), "GPU tests need an MI355X"
+    from paper_2411_10948_amd import mx, shiftquant
+    shiftquant.load()
+    return mx
+
+
+def _dtype(name):
+    import torch
+    return {"f32": torch.float32, "bf16": torch.bfloat16}[name]
+
+
+def _rand(rng, shape, dtype, spread=1.0):
+    """(tensor on the GPU, its values in float64)"""
+    import torch
+    x = (rng.standard_normal(shape) * np.exp(rng.normal(0, spread, (shape[-1],)))).astype(np.float32)
+    t = torch.from_numpy(x).cuda().to(_dtype(dtype))
+    return t, t.double().cpu().numpy()
+
+
+def _check_matrix(m, want_codes, want_scales, rows, cols, at=0):
+    """Codes and scales of a matrix (in place `at` of a stack) equal to the reference's [rows, blocks, 32]."""
+    codes, scales = m.codes.view(max(m.stack, 1), -1)[at].cpu().numpy(), m.scales.view(max(m.stack, 1), -1)[at].cpu().numpy()
+    c, s = ref.mx_unpack(codes, scales, rows, cols)
+    np.testing.assert_array_equal(s, np.repeat(want_scales, 32, -1)[:, :cols])
+    np.testing.assert_array_equal(c, want_codes.reshape(rows, -1)[:, :cols])
+
+
+def _close(got, want, mag, K, dtype):
+    """Within the error of an fp32 sum of K exact products in any order (at most 2^-23 of the running sum for each
+    addition, were they cut and not rounded), and one rounding to bf16."""
+    tol = mag * (K + 2) * 2.0 ** -23
+    if dtype == "bf16":
+        tol = tol + (np.abs(want) + tol) * 2.0 ** -8
+    bad = ~(np.abs(got - want) <= tol)
+    assert not bad.any(), f"{bad.sum()} of {bad.size} off, worst {np.nanmax(np.abs(got - want) / np.maximum(tol, 1e-300))}"
+
+
+# ---------------------------------------------------------------------------
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("M,C", [(1, 1), (1, 32), (3, 33), (16, 128), (31, 130), (128, 64), (129, 511), (130, 520), (257, 96),
+                                 (700, 1030)])
+def test_quantize_both_axes(mx, M, C, dtype):
+    x, v = _rand(np.random.default_rng(M * 1009 + C), (M, C), dtype, 3.0)
+    a, t = mx.quantize(x, True, True)
+    _check_matrix(a, *ref.mx_codes(v), M, C)
+    _check_matrix(t, *ref.mx_codes(v.T), C, M)
+    only_rows, none = mx.quantize(x, True, False)
+    assert none is None and (only_rows.values() == a.values()).all()
+    _, only_cols = mx.quantize(x, False, True)
+    assert (only_cols.values() == t.values()).all()
+    np.testing.assert_array_equal(a.values().double().cpu().numpy(), ref.mx_values(v))
+    np.testing.assert_array_equal(a.values(_dtype("bf16")).double().cpu().numpy(), ref.mx_values(v))
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_quantize_ties_extremes_and_nonfinite(mx, dtype):
+    import torch
+    x = np.zeros((40, 64), np.float32)
+    x[0, :8] = [7.0, 5.0, 3.5, 2.5, 1.75, 1.25, 0.75, 0.25]
+    x[1] = -x[0]
+    x[2, :3] = [7.03125, -7.0, 6.96875]                  # just past, at and below the carry (exact in bf16)
+    x[3] = 2.0 ** -126
+    x[4] = 2.0 ** -133                                   # subnormal in fp32 and bf16
+    x[5] = 3.3895313892515355e38                         # bf16's largest
+    x[6, 5] = np.inf
+    x[7, 40] = -np.inf
+    x[8, 63] = np.nan
+    x[9] = -0.0
+    x[10, 0], x[10, 1] = 2.0 ** 100, 2.0 ** -100
+    x[11:, :] = np.random.default_rng(0).integers(-28, 29, (29, 64)) * 0.25      # many ties
+    t = torch.from_numpy(x).cuda().to(_dtype(dtype))
+    v = t.double().cpu().numpy()
+    a, tr = mx.quantize(t, True, True)
+    for m, want, r, c in ((a, v, 40, 64), (tr, v.T, 64, 40)):
+        k, s = ref.mx_codes(want)
+        _check_matrix(m, np.where(s[..., None] == 255, 0, k), s, r, c)
+        np.testing.assert_array_equal(m.values().double().cpu().numpy(), ref.mx_values(want))
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("shift,pad", [(0, 1), (1, 0), (3, 5), (8, 8)])
+def test_quantize_strided_and_misaligned(mx, dtype, shift, pad):
+    import torch
+    M, C = 70, 200
+    base, _ = _rand(np.random.default_rng(5), (M * (C + pad) + shift + C, 1), dtype)
+    x = base.view(-1)[shift:].as_strided((M, C), (C + pad, 1))
+    v = x.double().cpu().numpy()
+    a, t = mx.quantize(x, True, True)
+    _check_matrix(a, *ref.mx_codes(v), M, C)
+    _check_matrix(t, *ref.mx_codes(v.T), C, M)
+    assert isinstance(a.codes, torch.Tensor)
+
+
+def test_quantize_stack_of_weights(mx):
+    x, v = _rand(np.random.default_rng(6), (3, 40, 150), "bf16")
+    a, t = mx.quantize(x, True, True)
+    for e in range(3):
+        _check_matrix(a, *ref.mx_codes(v[e]), 40, 150, e)
+        _check_matrix(t, *ref.mx_codes(v[e].T), 150, 40, e)
+    np.testing.assert_array_equal(a.values().double().cpu().numpy(), ref.mx_values(v))
+
+
+OFFSETS = {
+    "even": [0, 64, 128, 192, 256],
+    "ragged": [0, 1, 1, 130, 131, 256],
+    "one expert has all": [0, 0, 256, 256],
+    "rows outside": [5, 37, 37, 200],
+    "one expert": [0, 256],
+    "many, most empty": [0] * 70 + [3] * 30 + [250] * 40 + [256],
+    "none has any": [17, 17, 17],
+}
+
+
+def _offsets(name):
+    import torch
+    off = OFFSETS[name]
+    return off, torch.tensor(off, dtype=torch.int32, device="cuda")
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("name", list(OFFSETS))
+def test_quantize_by_expert(mx, name, dtype):
+    M, C = 256, 72
+    off, o = _offsets(name)
+    x, v = _rand(np.random.default_rng(7), (M, C), dtype)
+    a, t = mx.quantize(x, True, True, o)
+    codes, scales = ref.mx_unpack(a.codes.view(-1).cpu().numpy(), a.scales.view(-1).cpu().numpy(), M, C)
+    k, s = ref.mx_codes(v)
+    rows = np.arange(off[0], off[-1])
+    np.testing.assert_array_equal(codes[rows], k.reshape(M, -1)[rows, :C])
+    np.testing.assert_array_equal(scales[rows], np.repeat(s, 32, -1)[rows, :C])
+    codes, scales = ref.mx_unpack(t.codes.view(-1).cpu().numpy(), t.scales.view(-1).cpu().numpy(), C, t.cols)
+    at = 0
+    for lo, hi in ref.segments(off):
+        if hi > lo:
+            k, s = ref.mx_codes(v[lo:hi].T)
+            n = hi - lo
+            np.testing.assert_array_equal(codes[:, at:at + n], k.reshape(C, -1)[:, :n])
+            np.testing.assert_array_equal(scales[:, at:at + n], np.repeat(s, 32, -1)[:, :n])
+            pad = -n % 128
+            assert not codes[:, at + n:at + n + pad].any()      # zeros up to the next 128
+        at += -(-(hi - lo) // 512) * 512
+
+
+# ---------------------------------------------------------------------------
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("M,N,K", [(1, 1, 1), (1, 17, 128), (16, 16, 32), (17, 33, 129), (64, 64, 512), (65, 100, 640),
+                                   (100, 130, 1000), (128, 256, 384), (200, 64, 8192), (300, 260, 2100), (33, 1000, 4096),
+                                   (520, 500, 260)])
+def test_gemm(mx, M, N, K, dtype):
+    import torch
+    rng = np.random.default_rng(M + 7 * N + 13 * K)
+    x, xv = _rand(rng, (M, K), "f32")
+    w, wv = _rand(rng, (N, K), "f32")
+    a, b = mx.quantize(x)[0], mx.quantize(w)[0]
+    C = torch.full((M, N + 3), 7.0, dtype=_dtype(dtype), device="cuda")
+    ws = mx._workspace(mx.sq_mx_gemm_workspace_size(M, N, K), "cuda")
+    mx.sq_mx_gemm(a.codes, a.scales, b.codes, b.scales, K, C[:, :N], ws)
+    want, mag = ref.mx_product(ref.mx_values(xv), ref.mx_values(wv))
+    _close(C[:, :N].double().cpu().numpy(), want, mag, K, dtype)
+    assert (C[:, N:] == 7.0).all()
+
+
+@pytest.mark.parametrize("M,N,K", [(2300, 2050, 700), (1024, 1100, 300), (8192, 40, 520), (700, 3000, 520)])
+def test_gemm_of_many_tiles(mx, M, N, K):
+    # every tile shape, checked on rows and columns at the edges and inside
+    import torch
+    rng = np.random.default_rng(M + N)
+    x, _ = _rand(rng, (M, K), "f32")
+    w, _ = _rand(rng, (N, K), "f32")
+    a, b = mx.quantize(x)[0], mx.quantize(w)[0]
+    C = torch.full((M, N), 7.0, device="cuda")
+    ws = mx._workspace(mx.sq_mx_gemm_workspace_size(M, N, K), "cuda")
+    mx.sq_mx_gemm(a.codes, a.scales, b.codes, b.scales, K, C, ws)
+    av, bv = a.values().double().cpu().numpy(), b.values().double().cpu().numpy()
+    want, mag = ref.mx_product(av, bv)
+    _close(C.double().cpu().numpy(), want, mag, K, "f32")
+
+
+def test_gemm_scales_of_every_size(mx):
+    # scales from 2^-127 up: products underflow to zero or overflow as fp32 does
+    import torch
+    x = torch.zeros(16, 64, device="cuda")
+    x[:, 0] = 2.0 ** torch.arange(-140.0, 116.0, 16.0, dtype=torch.float64, device="cuda").float()
+    w = torch.ones(16, 64, device="cuda")
+    a, b = mx.quantize(x)[0], mx.quantize(w)[0]
+    C = torch.empty(16, 16, device="cuda")
+    mx.sq_mx_gemm(a.codes, a.scales, b.codes, b.scales, 64, C)
+    want = a.values().double()[:, :1].expand(16, 16)
+    normal = want >= 2.0 ** -126
+    assert torch.equal(C.double()[normal], want[normal])
+    assert (C.double() - want).abs()[~normal].max() <= 2.0 ** -126
+
+
+@pytest.mark.parametrize("M", [1, 5, 16, 40])
+def test_nan_block_reaches_its_row_and_column_only(mx, M):
+    rng = np.random.default_rng(8)
+    N, K = 48, 300
+    x, _ = _rand(rng, (M, K), "f32")
+    w, _ = _rand(rng, (N, K), "f32")
+    x[M // 2, 70] = float("inf")
+    w[9, 299] = float("nan")
+    plan = mx.LinearPlan(M, K, N, dtype=_dtype("f32"))
+    got = plan.forward(x, mx.quantize(w)[0]).isnan().cpu().numpy()
+    want = np.zeros((M, N), bool)
+    want[M // 2] = True
+    want[:, 9] = True
+    np.testing.assert_array_equal(got, want)
+
+
+# ---------------------------------------------------------------------------
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("M,K,N", [(1, 4096, 64), (1, 1, 1), (2, 100, 33), (7, 1000, 130), (16, 520, 48), (16, 2048, 1000),
+                                   (17, 520, 48), (37, 1100, 200), (130, 600, 300)])
+def test_linear_forward(mx, M, K, N, dtype):
+    rng = np.random.default_rng(M + K + N)
+    x, xv = _rand(rng, (M, K), dtype)
+    w, wv = _rand(rng, (N, K), "bf16")
+    plan = mx.LinearPlan(M, K, N, dtype=_dtype(dtype))
+    y = plan.forward(x, mx.quantize(w)[0])
+    want, mag = ref.mx_product(ref.mx_values(xv), ref.mx_values(wv))
+    _close(y.double().cpu().numpy(), want, mag, K, dtype)
+
+
+def test_linear_strided_input(mx):
+    rng = np.random.default_rng(3)
+    for M in (3, 50):
+        big, _ = _rand(rng, (M, 700), "bf16")
+        x = big[:, 5:605]
+        w, wv = _rand(rng, (40, 600), "bf16")
+        plan = mx.LinearPlan(M, 600, 40)
+        want, mag = ref.mx_product(ref.mx_values(x.double().cpu().numpy()), ref.mx_values(wv))
+        _close(plan.forward(x, mx.quantize(w)[0]).double().cpu().numpy(), want, mag, 600, "bf16")
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("M,C_in,C_out", [(1, 32, 32), (45, 100, 70), (130, 64, 200), (600, 260, 33), (1000, 130, 520)])
+def test_linear_training_step(mx, M, C_in, C_out, dtype):
+    rng = np.random.default_rng(M)
+    x, xv = _rand(rng, (M, C_in), dtype)
+    dy, dv = _rand(rng, (M, C_out), dtype)
+    w, wv = _rand(rng, (C_out, C_in), dtype)
+    plan = mx.LinearPlan(M, C_in, C_out, dtype=_dtype(dtype), train=True)
+    plan.quantize_weight(w)
+    y = plan.forward(x)
+    dx, dw = plan.backward(dy)
+    q = ref.mx_values
+    _close(y.double().cpu().numpy(), *ref.mx_product(q(xv), q(wv)), C_in, dtype)
+    _close(dx.double().cpu().numpy(), *ref.mx_product(q(dv), q(wv.T)), C_out, dtype)
+    _close(dw.double().cpu().numpy(), *ref.mx_product(q(dv.T), q(xv.T)), M, "f32")
+
+
+def test_gradients_against_differences(mx):
+    # The step's gradients are those of L = sum(dY * Y) with exact operands: on values that 4 bits hold exactly the
+    # products are linear in X and in W, so a difference of L over one element is the gradient itself.
+    import torch
+    rng = np.random.default_rng(4)
+    M, K, N = 48, 64, 40
+    hold = lambda *s: torch.from_numpy(rng.choice([-6, -4, -3, -2, -1.5, -1, -0.5, 0, 0.5, 1, 1.5, 2, 3, 4, 6], s)).float().cuda()
+    x, w, dy = hold(M, K), hold(N, K), hold(M, N)
+    for t in (x, w, dy):        # a 6 in every block of both axes: one scale everywhere
+        t[::8, ::8] = 6.0
+    for t in (x, w, dy):
+        a, tr = mx.quantize(t, True, True)
+        assert torch.equal(a.values(), t) and torch.equal(tr.values(), t.T)
+    plan = mx.LinearPlan(M, K, N, dtype=torch.float32, train=True)
+    loss = lambda x, w: (dy.double() * (plan.quantize_weight(w) or plan.forward(x)).double()).sum().item()
+    plan.quantize_weight(w)
+    plan.forward(x)
+    dx, dw = (t.clone() for t in plan.backward(dy))
+    for _ in range(6):
+        i, k, n = int(rng.integers(1, M)), int(rng.integers(1, K)), int(rng.integers(1, N))
+        for t, g, at in ((x, dx, (i | 1, k)), (w, dw, (n | 1, k))):
+            up, down = t.clone(), t.clone()
+            up[at], down[at] = 2.0, -2.0
+            d = (loss(up, w) - loss(down, w)) / 4 if t is x else (loss(x, up) - loss(x, down)) / 4
+            assert abs(d - g[at].item()) <= 1e-9 * max(1.0, abs(d))
+
+
+# ---------------------------------------------------------------------------
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("name", list(OFFSETS))
+@pytest.mark.parametrize("K,N", [(72, 40), (600, 130)])
+def test_experts_training_step(mx, name, dtype, K, N):
+    import torch
+    M = 256
+    off, o = _offsets(name)
+    E = len(off) - 1
+    rng = np.random.default_rng(len(name))
+    x, xv = _rand(rng, (M, K), dtype)
+    dy, dv = _rand(rng, (M, N), dtype)
+    w, wv = _rand(rng, (E, N, K), dtype)
+    plan = mx.LinearPlan(M, K, N, dtype=_dtype(dtype), experts=E, train=True)
+    plan.Y.fill_(7.0)
+    plan.dX.fill_(7.0)
+    plan.dW.fill_(float("nan"))
+    plan.quantize_weight(w)
+    y = plan.forward(x, offsets=o)
+    dx, dw = plan.backward(dy)
+    q = ref.mx_values
+    y, dx, dw = (t.double().cpu().numpy() for t in (y, dx, dw))
+    for e, (lo, hi) in enumerate(ref.segments(off)):
+        if hi > lo:
+            _close(y[lo:hi], *ref.mx_product(q(xv[lo:hi]), q(wv[e])), K, dtype)
+            _close(dx[lo:hi], *ref.mx_product(q(dv[lo:hi]), q(wv[e].T)), N, dtype)
+            _close(dw[e], *ref.mx_product(q(dv[lo:hi].T), q(xv[lo:hi].T)), hi - lo, "f32")
+        else:
+            assert not dw[e].any()
+    for r in (slice(0, off[0]), slice(off[-1], M)):     # rows of no expert
+        assert (y[r] == 7.0).all() and (dx[r] == 7.0).all()
+    assert isinstance(plan.offsets, torch.Tensor)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("M,E,K,N", [(1, 4, 100, 33), (8, 64, 512, 48), (30, 3, 1000, 130), (90, 2, 96, 70),
+                                     (1500, 5, 200, 300)])
+def test_experts_serving(mx, M, E, K, N, dtype):
+    # few rows an expert (one launch) and many
+    import torch
+    rng = np.random.default_rng(M)
+    x, xv = _rand(rng, (M, K), dtype)
+    w, wv = _rand(rng, (E, N, K), "bf16")
+    cut = np.sort(rng.integers(0, M + 1, E - 1))
+    off = [0, *cut.tolist(), M]
+    plan = mx.LinearPlan(M, K, N, dtype=_dtype(dtype), experts=E)
+    y = plan.forward(x, mx.quantize(w)[0], torch.tensor(off, dtype=torch.int32, device="cuda")).double().cpu().numpy()
+    for e, (lo, hi) in enumerate(ref.segments(off)):
+        if hi > lo:
+            _close(y[lo:hi], *ref.mx_product(ref.mx_values(xv[lo:hi]), ref.mx_values(wv[e])), K, dtype)
+
+
+@pytest.mark.parametrize("off", [[0, 300, 100, 256], [-5, 40, 900, 256], [200, 100, 50, 0]])
+def test_offsets_out_of_order_stay_in_the_buffers(mx, off):
+    # what is computed is unspecified; the words around every output must survive
+    import torch
+    M, K, N, E = 256, 96, 64, 3
+    rng = np.random.default_rng(1)
+    x, _ = _rand(rng, (M, K), "f32")
+    dy, _ = _rand(rng, (M, N), "f32")
+    w, _ = _rand(rng, (E, N, K), "f32")
+    o = torch.tensor(off, dtype=torch.int32, device="cuda")
+    plan = mx.LinearPlan(M, K, N, dtype=torch.float32, experts=E, train=True)
+    guard = {}
+    for key in ("Y", "dX", "dW"):
+        t = getattr(plan, key)
+        big = torch.full((t.numel() + 2048,), 5.0, device="cuda")
+        setattr(plan, key, big[1024:1024 + t.numel()].view(t.shape))
+        guard[key] = big
+    for m in (plan.x, plan.x_t, plan.dy, plan.dy_t):
+        for f in ("codes", "scales"):
+            t = getattr(m, f)
+            big = torch.full((t.numel() + 8192,), 5, dtype=torch.uint8, device="cuda")
+            setattr(m, f, big[4096:4096 + t.numel()].view(t.shape))
+            guard[id(m), f] = big
+    plan.quantize_weight(w)
+    plan.forward(x, offsets=o)
+    plan.backward(dy)
+    torch.cuda.synchronize()
+    for big in guard.values():
+        n = 1024 if big.dtype == torch.float32 else 4096
+        assert (big[:n] == 5).all() and (big[-n:] == 5).all()
+
+
+# ---------------------------------------------------------------------------
+def test_other_stream_and_determinism(mx):
+    import torch
+    rng = np.random.default_rng(2)
+    M, K, N, E = 700, 300, 200, 6
+    x, _ = _rand(rng, (M, K), "bf16")
+    dy, _ = _rand(rng, (M, N), "bf16")
+    w, _ = _rand(rng, (E, N, K), "bf16")
+    o = torch.tensor([0, 10, 10, 300, 301, 600, 700], dtype=torch.int32, device="cuda")
+    plan = mx.LinearPlan(M, K, N, experts=E, train=True)
+
+    def step(s=None):
+        plan.quantize_weight(w, s)
+        y = plan.forward(x, offsets=o, stream=s)
+        return (y, *plan.backward(dy, s))
+    first = [t.clone() for t in step()]
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    for t in (plan.Y, plan.dX, plan.dW):
+        t.fill_(float("nan"))
+    torch.cuda.synchronize()
+    again = step(s)
+    s.synchronize()
+    for a, b in zip(first, again):
+        assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("M,K,N,E,train", [(1, 512, 256, 0, False), (300, 1024, 200, 0, False), (256, 200, 100, 5, True),
+                                           (600, 300, 64, 0, True)])
+def test_graph_replay(mx, M, K, N, E, train):
+    import torch
+    rng = np.random.default_rng(9)
+    x, _ = _rand(rng, (M, K), "bf16")
+    dy, _ = _rand(rng, (M, N), "bf16")
+    w, _ = _rand(rng, (E, N, K) if E else (N, K), "bf16")
+    o = torch.tensor(sorted([0, M] + rng.integers(0, M + 1, E - 1).tolist()), dtype=torch.int32, device="cuda") if E else None
+    plan = mx.LinearPlan(M, K, N, experts=E, train=train)
+    codes = None if train else mx.quantize(w)[0]
+
+    def step(s=None):
+        if not train:
+            return (plan.forward(x, codes, o, s),)
+        plan.quantize_weight(w, s)
+        y = plan.forward(x, offsets=o, stream=s)
+        return (y, *plan.backward(dy, s))
+    want = [t.clone() for t in step()]
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    step(s)
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g, stream=s):
+        out = step(s)
+    for _ in range(3):
+        x2 = (x.float() * 2).to(x.dtype)        # the program's own work between replays
+        for t in out:
+            t.fill_(float("nan"))
+        torch.cuda.synchronize()
+        g.replay()
+        torch.cuda.synchronize()
+        for a, b in zip(out, want):
+            assert torch.equal(a, b)
+    assert x2 is not None
+
+
+def test_empty(mx):
+    import torch
+    plan = mx.LinearPlan(0, 64, 32, dtype=torch.float32, train=True)
+    plan.quantize_weight(torch.ones(32, 64, device="cuda"))
+    plan.dW.fill_(3.0)
+    assert plan.forward(torch.empty(0, 64, device="cuda")).shape == (0, 32)
+    dx, dw = plan.backward(torch.empty(0, 32, device="cuda"))
+    assert dx.shape == (0, 64) and not dw.any()         # a sum over no rows
+    plan = mx.LinearPlan(0, 64, 32, dtype=torch.float32, experts=3, train=True)
+    plan.quantize_weight(torch.ones(3, 32, 64, device="cuda"))
+    plan.dW.fill_(3.0)
+    plan.forward(torch.empty(0, 64, device="cuda"), offsets=torch.zeros(4, dtype=torch.int32, device="cuda"))
+    assert not plan.backward(torch.empty(0, 32, device="cuda"))[1].any()
