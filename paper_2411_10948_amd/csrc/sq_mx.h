@@ -161,14 +161,14 @@ __device__ __forceinline__ Segment find_segment(const int32_t* offsets, int expe
         if (hit) {
             const int src = __ffsll((unsigned long long)hit) - 1;
             r.expert = base + src;
-            r.lo = __shfl(lo, src);
-            r.hi = __shfl(hi, src);
-            r.tile = index - tiles - __shfl(ti - t, src);
-            r.inner = inner + (int64_t)__shfl(ki - k, src) * kMxUnit;
+            r.lo = __builtin_amdgcn_readlane(lo, src);
+            r.hi = __builtin_amdgcn_readlane(hi, src);
+            r.tile = index - tiles - __builtin_amdgcn_readlane(ti - t, src);
+            r.inner = inner + (int64_t)__builtin_amdgcn_readlane(ki - k, src) * kMxUnit;
             return r;
         }
-        tiles += __shfl(ti, 63);
-        inner += (int64_t)__shfl(ki, 63) * kMxUnit;
+        tiles += __builtin_amdgcn_readlane(ti, 63);
+        inner += (int64_t)__builtin_amdgcn_readlane(ki, 63) * kMxUnit;
     }
     return r;
 }
@@ -183,11 +183,11 @@ __device__ __forceinline__ void segment_inner(const int32_t* offsets, int expert
         segment_of(offsets, experts, rows, base + lane, lo, hi);
         const int k = (hi - lo + kMxUnit - 1) / kMxUnit, ki = wave_scan(k, lane);
         if (e < base + 64) {
-            inner += (int64_t)__shfl(ki - k, e - base) * kMxUnit;
-            len = __shfl(hi - lo, e - base);
+            inner += (int64_t)__builtin_amdgcn_readlane(ki - k, e - base) * kMxUnit;
+            len = __builtin_amdgcn_readlane(hi - lo, e - base);
             return;
         }
-        inner += (int64_t)__shfl(ki, 63) * kMxUnit;
+        inner += (int64_t)__builtin_amdgcn_readlane(ki, 63) * kMxUnit;
     }
 }
 

@@ -11,20 +11,67 @@ namespace sq {
 
 namespace {
 
-typedef float v4f __attribute__((ext_vector_type(4)));
+typedef __bf16 v2bf __attribute__((ext_vector_type(2)));
+typedef uint16_t v2u16 __attribute__((ext_vector_type(2)));
 
-// codes of 8 values already divided by their scale, element 0 in the low bits
-__device__ __forceinline__ uint32_t codes8(const float* v) {
+// Codes of 8 values, element 0 in the low bits.  The conversion divides by the
+// scale and rounds once (to the nearest even, saturating), for every scale
+// 2^-127 .. 2^126 and subnormal inputs too.
+__device__ __forceinline__ uint32_t codes8(const float* v, float scale) {
     uint32_t r = 0;
-    r = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(r, v[0], v[1], 1.0f, 0);
-    r = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(r, v[2], v[3], 1.0f, 1);
-    r = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(r, v[4], v[5], 1.0f, 2);
-    r = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(r, v[6], v[7], 1.0f, 3);
+    r = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(r, v[0], v[1], scale, 0);
+    r = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(r, v[2], v[3], scale, 1);
+    r = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(r, v[4], v[5], scale, 2);
+    r = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(r, v[6], v[7], scale, 3);
     return r;
+}
+__device__ __forceinline__ v2bf as_bf16(uint32_t w) {
+    v2bf b;
+    __builtin_memcpy(&b, &w, 4);
+    return b;
+}
+__device__ __forceinline__ uint32_t codes8(uint32_t a, uint32_t b, uint32_t c, uint32_t d, float scale) {   // bf16 pairs
+    uint32_t r = 0;
+    r = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(r, as_bf16(a), scale, 0);
+    r = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(r, as_bf16(b), scale, 1);
+    r = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(r, as_bf16(c), scale, 2);
+    r = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(r, as_bf16(d), scale, 3);
+    return r;
+}
+// running maximum of the magnitudes of two bf16 at once
+__device__ __forceinline__ uint32_t pair_max(uint32_t m, uint32_t w) {
+    v2u16 a, b;
+    w &= 0x7FFF7FFFu;
+    __builtin_memcpy(&a, &m, 4);
+    __builtin_memcpy(&b, &w, 4);
+    a = __builtin_elementwise_max(a, b);
+    __builtin_memcpy(&m, &a, 4);
+    return m;
+}
+
+template <int CTRL>
+__device__ __forceinline__ uint32_t quad(uint32_t v) {
+    return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, CTRL, 0xF, 0xF, false);
+}
+constexpr int kXor1 = 0xB1, kXor2 = 0x4E;   // quad_perm [1,0,3,2], [2,3,0,1]
+
+// c[i] of lane j of a quad to c[j] of lane i.
+__device__ __forceinline__ void transpose4(uint32_t* c, int lane) {
+    const bool odd = lane & 1, high = lane & 2;
+#pragma unroll
+    for (int i = 0; i < 4; i += 2) {
+        const uint32_t got = quad<kXor1>(odd ? c[i] : c[i + 1]);
+        c[odd ? i : i + 1] = got;
+    }
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        const uint32_t got = quad<kXor2>(high ? c[i] : c[i + 2]);
+        c[high ? i : i + 2] = got;
+    }
 }
 
 // Tile of a quantizer block: 128 rows x TC columns, in LDS as they came, for
-// both directions.  128 rows are one tile of the transpose's inner axis.
+// the transpose; 128 rows are one tile of the transpose's inner axis.
 template <typename T>
 struct QuantTile;
 template <>
@@ -36,24 +83,23 @@ struct QuantTile<uint16_t> {   // bf16 bits
     static constexpr int TC = 128;
 };
 
-template <typename T>
-__device__ __forceinline__ float value_of(T v);
-template <>
-__device__ __forceinline__ float value_of<float>(float v) { return v; }
-template <>
-__device__ __forceinline__ float value_of<uint16_t>(uint16_t v) { return bf16_value(v); }
-
-// Eight lanes (fp32) or sixteen (bf16) hold a row of the tile, 8 elements
-// each, so a block of 32 is four lanes' and its maximum two exchanges away.
-// The transposed direction reads the tile's columns from LDS, one word (one
-// or two columns) a lane.
+// A wave takes 32 rows of the tile; a row is 8 lanes' (fp32) or 16 lanes'
+// (bf16), 8 elements each, so a block of 32 is a quad's and its maximum two
+// exchanges away.  After four passes over the rows the quad's codes are
+// transposed among its lanes: a lane then holds a whole block, and the wave's
+// 16-byte stores cover whole 1 KB tiles.  The other direction reads the tile's
+// columns from LDS, one word (one or two columns) a lane.  bf16 stays packed
+// from load to code (maximum, conversion), which halves the instructions;
+// vector instructions bound the kernel, not HBM, when each element was
+// unpacked and multiplied by the scale's inverse (8192 x 11008 both ways 84 us).
 template <typename T>
 __global__ __launch_bounds__(256) void k_mx_quantize(MxQuantArgs p, int64_t tiles_c, bool vec) {
-    constexpr int TC = QuantTile<T>::TC, kLanes = TC / 8, kPass = 256 / kLanes, kPasses = 128 / kPass;
+    constexpr int TC = QuantTile<T>::TC, kLanes = TC / 8, kPass = 64 / kLanes, kPasses = 32 / kPass;
+    constexpr int kWords = 8 * sizeof(T) / 4;            // words a lane loads of a row
     constexpr int kCols = 4 / sizeof(T);                 // columns a lane takes of the transpose
-    __shared__ __attribute__((aligned(16))) T tile[128][TC];
+    __shared__ __attribute__((aligned(16))) uint32_t tile[128][TC * sizeof(T) / 4];
 
-    const int tid = threadIdx.x;
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const int64_t tr = blockIdx.x / tiles_c, tc = blockIdx.x - tr * tiles_c, mat = blockIdx.y;
     int64_t row0 = tr * 128, row_end = p.rows, inner = row0;
     if (p.offsets) {
@@ -66,87 +112,117 @@ __global__ __launch_bounds__(256) void k_mx_quantize(MxQuantArgs p, int64_t tile
     const int64_t col0 = tc * TC;
     const T* x = static_cast<const T*>(p.x) + mat * p.stride;
 
-    const int q = tid % kLanes, r0 = tid / kLanes;
+    const int q = lane % kLanes, r0 = wave * 32 + lane / kLanes;
     const int64_t c = col0 + 8 * q;
-    T v[kPasses][8];
+    uint32_t v[kPasses][kWords];
 #pragma unroll
     for (int i = 0; i < kPasses; ++i) {
         const int64_t r = row0 + r0 + i * kPass;
         const T* src = x + r * p.ld + c;
         if (r < row_end && vec && c + 8 <= p.cols) {
 #pragma unroll
-            for (int w = 0; w < (int)(8 * sizeof(T) / 16); ++w)
-                reinterpret_cast<uint4*>(v[i])[w] = reinterpret_cast<const uint4*>(src)[w];
+            for (int w = 0; w < kWords; w += 4)
+                *reinterpret_cast<uint4*>(&v[i][w]) = *reinterpret_cast<const uint4*>(src + w * 4 / sizeof(T));
         } else {
+            T t[8];
 #pragma unroll
-            for (int e = 0; e < 8; ++e) v[i][e] = r < row_end && c + e < p.cols ? src[e] : (T)0;
+            for (int e = 0; e < 8; ++e) t[e] = r < row_end && c + e < p.cols ? src[e] : (T)0;
+            __builtin_memcpy(v[i], t, sizeof(t));
         }
+    }
+    if (p.codes_t) {
+#pragma unroll
+        for (int i = 0; i < kPasses; ++i)
+#pragma unroll
+            for (int w = 0; w < kWords; w += 4)
+                *reinterpret_cast<uint4*>(&tile[r0 + i * kPass][q * kWords + w]) =
+                    make_uint4(v[i][w], v[i][w + 1], v[i][w + 2], v[i][w + 3]);
     }
     if (p.codes) {
         const int64_t units = mx_units(p.cols);
         uint8_t* codes = p.codes + mat * mx_groups(p.rows) * units * kMxUnitBytes;
         uint8_t* scales = p.scales + mat * mx_groups(p.rows) * units * kMxUnitScales;
+        const int blk = (int)(c >> 5) & 3;
+        codes += (c >> 7) * kMxTileBytes + blk * 256;
+        scales += (c >> 9) * kMxUnitScales + blk * 64 + ((c >> 7) & 3);
 #pragma unroll
-        for (int i = 0; i < kPasses; ++i) {
-            const int64_t r = row0 + r0 + i * kPass;
-            float f[8];
-            uint32_t b = 0;
+        for (int i = 0; i < kPasses; i += 4) {
+            uint32_t k[4], s[4];
 #pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                f[e] = value_of<T>(v[i][e]);
-                b = max(b, __float_as_uint(f[e]) & 0x7FFFFFFFu);
+            for (int j = 0; j < 4; ++j) {
+                const uint32_t* w = v[i + j];
+                uint32_t b = 0;
+                if constexpr (sizeof(T) == 4) {
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) b = max(b, w[e] & 0x7FFFFFFFu);
+                } else {
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) b = pair_max(b, w[e]);
+                    b = max(b << 16, b & 0xFFFF0000u);
+                }
+                b = max(b, quad<kXor1>(b));
+                b = max(b, quad<kXor2>(b));
+                s[j] = mx_scale4(b);
+                const float scale = mx_value(s[j]);
+                if constexpr (sizeof(T) == 4) {
+                    float f[8];
+                    __builtin_memcpy(f, w, sizeof(f));
+                    k[j] = codes8(f, scale);
+                } else {
+                    k[j] = codes8(w[0], w[1], w[2], w[3], scale);
+                }
+                k[j] = s[j] == 255u ? 0u : k[j];
             }
-            b = max(b, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)b, 0xB1, 0xF, 0xF, false));   // lane ^ 1
-            b = max(b, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)b, 0x4E, 0xF, 0xF, false));   // lane ^ 2
-            const uint32_t s = mx_scale4(b);
-            const float inv = mx_inverse(s);
-#pragma unroll
-            for (int e = 0; e < 8; ++e) f[e] = s == 255u ? 0.0f : f[e] * inv;
+            transpose4(k, lane);
+            const int j = lane & 3;
+            const int64_t r = row0 + r0 + (i + j) * kPass, group = (r >> 4) * units;
+            const int slot = (int)(r & 15);
             if (r < row_end) {
-                const int64_t group = r >> 4;
-                const int slot = (int)(r & 15), blk = (int)(c >> 5) & 3;
-                *reinterpret_cast<uint32_t*>(codes + (group * units * 4 + (c >> 7)) * kMxTileBytes + blk * 256 + slot * 16 +
-                                             (q & 3) * 4) = codes8(f);
-                if ((q & 3) == 0)
-                    scales[(group * units + (c >> 9)) * kMxUnitScales + blk * 64 + slot * 4 + ((c >> 7) & 3)] = (uint8_t)s;
+                *reinterpret_cast<uint4*>(codes + group * kMxUnitBytes + slot * 16) = make_uint4(k[0], k[1], k[2], k[3]);
+                scales[group * kMxUnitScales + slot * 4] = (uint8_t)(j & 2 ? (j & 1 ? s[3] : s[2]) : (j & 1 ? s[1] : s[0]));
             }
         }
     }
     if (!p.codes_t) return;
-#pragma unroll
-    for (int i = 0; i < kPasses; ++i)
-#pragma unroll
-        for (int w = 0; w < (int)(8 * sizeof(T) / 16); ++w)
-            reinterpret_cast<uint4*>(&tile[r0 + i * kPass][8 * q])[w] = reinterpret_cast<uint4*>(v[i])[w];
     __syncthreads();
     if (inner + 128 > p.cap_t) return;   // offsets out of order
     const int64_t units = mx_units(p.cap_t);
-    uint8_t* codes = p.codes_t + mat * mx_groups(p.cols) * units * kMxUnitBytes;
-    uint8_t* scales = p.scales_t + mat * mx_groups(p.cols) * units * kMxUnitScales;
-    const int word = tid & 63, blk = tid >> 6;
-    uint32_t w[32];
+    uint8_t* codes = p.codes_t + mat * mx_groups(p.cols) * units * kMxUnitBytes + (inner >> 7) * kMxTileBytes + wave * 256;
+    uint8_t* scales = p.scales_t + mat * mx_groups(p.cols) * units * kMxUnitScales + (inner >> 9) * kMxUnitScales + wave * 64 +
+                      ((inner >> 7) & 3);
+    uint32_t w[32], m = 0;
 #pragma unroll
-    for (int i = 0; i < 32; ++i) w[i] = reinterpret_cast<const uint32_t*>(&tile[32 * blk + i][0])[word];
+    for (int i = 0; i < 32; ++i) {
+        w[i] = tile[32 * wave + i][lane];
+        if constexpr (sizeof(T) == 4) m = max(m, w[i] & 0x7FFFFFFFu);
+        else m = pair_max(m, w[i]);
+    }
 #pragma unroll
     for (int h = 0; h < kCols; ++h) {
-        const int64_t col = col0 + word * kCols + h;
-        float f[32];
-        uint32_t b = 0;
+        const int64_t col = col0 + lane * kCols + h;
+        const uint32_t s = mx_scale4(kCols == 1 ? m : (h ? m & 0xFFFF0000u : m << 16));
+        const float scale = mx_value(s);
+        uint32_t k[4];
 #pragma unroll
-        for (int i = 0; i < 32; ++i) {
-            f[i] = kCols == 1 ? __uint_as_float(w[i]) : __uint_as_float(h ? w[i] & 0xFFFF0000u : w[i] << 16);
-            b = max(b, __float_as_uint(f[i]) & 0x7FFFFFFFu);
+        for (int i = 0; i < 4; ++i) {
+            if constexpr (kCols == 1) {
+                float f[8];
+                __builtin_memcpy(f, w + 8 * i, sizeof(f));
+                k[i] = codes8(f, scale);
+            } else {
+                uint32_t t[4];   // two rows' elements of this column
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    t[e] = __builtin_amdgcn_perm(w[8 * i + 2 * e + 1], w[8 * i + 2 * e], h ? 0x07060302u : 0x05040100u);
+                k[i] = codes8(t[0], t[1], t[2], t[3], scale);
+            }
+            k[i] = s == 255u ? 0u : k[i];
         }
-        const uint32_t s = mx_scale4(b);
-        const float inv = mx_inverse(s);
-#pragma unroll
-        for (int i = 0; i < 32; ++i) f[i] = s == 255u ? 0.0f : f[i] * inv;
         if (col < p.cols) {
-            const int64_t group = col >> 4;
+            const int64_t group = (col >> 4) * units;
             const int slot = (int)(col & 15);
-            *reinterpret_cast<uint4*>(codes + (group * units * 4 + (inner >> 7)) * kMxTileBytes + blk * 256 + slot * 16) =
-                make_uint4(codes8(f), codes8(f + 8), codes8(f + 16), codes8(f + 24));
-            scales[(group * units + (inner >> 9)) * kMxUnitScales + blk * 64 + slot * 4 + ((inner >> 7) & 3)] = (uint8_t)s;
+            *reinterpret_cast<uint4*>(codes + group * kMxUnitBytes + slot * 16) = make_uint4(k[0], k[1], k[2], k[3]);
+            scales[group * kMxUnitScales + slot * 4] = (uint8_t)s;
         }
     }
 }

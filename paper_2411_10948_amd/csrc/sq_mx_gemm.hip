@@ -9,6 +9,7 @@
 // from memory to LDS and from LDS to registers in lane order: contiguous
 // 1 KB loads and conflict-free reads, no swizzle.
 #include <algorithm>
+#include <cstdlib>
 #include <type_traits>
 
 #include "sq_mx.h"
@@ -39,23 +40,26 @@ __device__ __forceinline__ void wait_loads() {
     __builtin_amdgcn_s_waitcnt((N & 0xF) | ((N >> 4) << 14) | (0x7 << 4));
 }
 
-// Block tile BM x BN of WM x WN waves, four stages of 128 inner elements in
-// LDS and two of the scales of 512.
-template <int BM_, int BN_, int WM_, int WN_>
+// Block tile BM x BN of WM x WN waves, a ring of STAGES stages of 128 inner
+// elements in LDS.
+template <int BM_, int BN_, int WM_, int WN_, int STAGES_>
 struct MxCfg {
-    static constexpr int BM = BM_, BN = BN_, WM = WM_, WN = WN_, STAGES = 4;
+    static constexpr int BM = BM_, BN = BN_, WM = WM_, WN = WN_, STAGES = STAGES_;
     static constexpr int kWaves = WM * WN, kThreads = 64 * kWaves;
     static constexpr int TM = BM / WM, TN = BN / WN, FM = TM / 16, FN = TN / 16;
     static constexpr int kGroups = (BM + BN) / 16;            // 16-row operand groups of a stage
     static constexpr int LPW = kGroups / kWaves;              // 1 KB loads per wave per stage
     static constexpr int kStage = kGroups * kMxTileBytes;
-    static constexpr int kScales = kGroups * kMxUnitScales;
-    static constexpr int kSmem = STAGES * kStage + 2 * kScales;
+    static constexpr int kSmem = STAGES * kStage;
+    static constexpr int kCycle = STAGES == 3 ? 24 : 8;       // steps after which stage, buffer and scale byte recur
     static_assert(LPW * kWaves == kGroups && TM % 16 == 0 && TN % 16 == 0, "even split");
+    static_assert(BM / 16 % kWaves == 0 && BN / 16 % kWaves == 0, "a wave's i-th loads are all of A or all of B");
+    static_assert(STAGES == 3 || STAGES == 4, "ring");
 };
-using MxLarge = MxCfg<256, 256, 4, 2>;   // 8 waves of 64 x 128, 144 KB: one block per CU
-using MxMid = MxCfg<128, 128, 2, 2>;     // 4 waves of 64 x 64, 72 KB: two
-using MxSmall = MxCfg<64, 64, 2, 2>;     // 4 waves of 32 x 32, 36 KB: four
+using MxLarge = MxCfg<256, 256, 4, 2, 3>;   // 8 waves of 64 x 128, 96 KB: one block per CU
+using MxDuo = MxCfg<256, 128, 4, 1, 3>;     // 4 waves of 64 x 128, 72 KB: two
+using MxMid = MxCfg<128, 128, 2, 2, 3>;     // 4 waves of 64 x 64, 48 KB: three
+using MxSmall = MxCfg<64, 64, 2, 2, 4>;     // 4 waves of 32 x 32, 32 KB: five
 
 [[maybe_unused]] constexpr int64_t kXcds = 8, kGroupM = 8;
 
@@ -68,6 +72,14 @@ using MxSmall = MxCfg<64, 64, 2, 2>;     // 4 waves of 32 x 32, 36 KB: four
 __device__ __forceinline__ void store_out(void* C, int type, int64_t at, float v) {
     if (type == SQ_TYPE_F32) static_cast<float*>(C)[at] = v;
     else static_cast<uint16_t*>(C)[at] = (uint16_t)bf16_bits(v);
+}
+
+// f(0), f(1), ... f(N - 1) as compile-time constants, until one returns false.
+template <int N, int I = 0, class F>
+__device__ __forceinline__ void unrolled_steps(F f) {
+    if constexpr (I < N) {
+        if (f(std::integral_constant<int, I>())) unrolled_steps<N, I + 1>(f);
+    }
 }
 
 template <class T, int MODE>
@@ -109,52 +121,41 @@ __global__ __launch_bounds__(T::kThreads, 2) void k_mx_gemm(MxGemmArgs p, int64_
         n0 = (u / gsz) * T::BN;
     }
 
-    // ---- operand loads: fixed per-lane offsets, a scalar along the inner axis ----
-    // Group g of a stage: rows 16 g.. of A (g < BM / 16), then of B; rows past
-    // the end read the last one, whose results are never stored.
+    // ---- operand loads: a fixed offset per lane, the group and the inner axis in a scalar ----
+    // Group g of a stage: rows 16 g.. of A (g < BM / 16), then of B; groups
+    // past the last one read it again, their results are never stored.  A's
+    // rows may start inside a 16-row group (kExpertRows): then the lanes of its
+    // later rows read one group further.
     const int64_t units = mx_units(p.K), gbytes = units * kMxUnitBytes, sbytes = units * kMxUnitScales;
-    const uint8_t* A = p.A + (m0 >> 4) * gbytes;
-    const uint8_t* As = p.As + (m0 >> 4) * sbytes;
     const int64_t bm = MODE == kExpertRows ? expert * mx_groups(p.N) : 0;
-    const uint8_t* B = p.B + (bm + (n0 >> 4)) * gbytes;
-    const uint8_t* Bs = p.Bs + (bm + (n0 >> 4)) * sbytes;
-    const int64_t groups_a = mx_groups(p.M) - (m0 >> 4), groups_b = mx_groups(p.N) - (n0 >> 4);
     auto rsrc = [](const uint8_t* base, int64_t bytes) {
         return __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(base), (short)0,
                                                  (int)min(bytes, (int64_t)0x7FFFFFFF), 0x00020000);
     };
-    const __amdgpu_buffer_rsrc_t rA = rsrc(A, groups_a * gbytes), rB = rsrc(B, groups_b * gbytes),
-                                 rAs = rsrc(As, groups_a * sbytes), rBs = rsrc(Bs, groups_b * sbytes);
-    uint32_t off[T::LPW], soff[T::LPW];
-#pragma unroll
-    for (int i = 0; i < T::LPW; ++i) {
-        const int g = i * T::kWaves + wave;
-        const bool isa = g < T::BM / 16;
-        const int64_t first = isa ? m0 : n0, last = (isa ? p.M : p.N) - 1;
-        const int64_t r = min(first + 16 * (isa ? g : g - T::BM / 16) + (lane & 15), last);
-        const uint32_t grp = (uint32_t)((r >> 4) - (first >> 4)), slot = (uint32_t)(r & 15);
-        off[i] = grp * (uint32_t)gbytes + (uint32_t)(lane >> 4) * 256 + slot * 16;
-        soff[i] = grp * (uint32_t)sbytes + (uint32_t)(lane >> 4) * 64 + slot * 4;
-    }
-    auto issue = [&](int t) {
-        const int64_t at = t0 + t;
-        if ((t & 3) == 0) {
-            uint8_t* ss = smem + T::STAGES * T::kStage + ((t >> 2) & 1) * T::kScales;
-            const int k = (int)(at >> 2) * kMxUnitScales;
-#pragma unroll
-            for (int i = 0; i < T::LPW; ++i) {
-                const int g = i * T::kWaves + wave;
-                __builtin_amdgcn_raw_ptr_buffer_load_lds(g < T::BM / 16 ? rAs : rBs, (lds_void_t*)(ss + g * kMxUnitScales), 4,
-                                                         soff[i], k, 0, 0);
-            }
-        }
-        uint8_t* st = smem + (t & 3) * T::kStage;
-        const int k = (int)at * kMxTileBytes;
+    const int last_a = (int)(mx_groups(p.M) - 1 - (m0 >> 4)), last_b = (int)(mx_groups(p.N) - 1 - (n0 >> 4));
+    const __amdgpu_buffer_rsrc_t rA = rsrc(p.A + (m0 >> 4) * gbytes, (last_a + 1) * gbytes),
+                                 rB = rsrc(p.B + (bm + (n0 >> 4)) * gbytes, (last_b + 1) * gbytes),
+                                 rAs = rsrc(p.As + (m0 >> 4) * sbytes, (last_a + 1) * sbytes),
+                                 rBs = rsrc(p.Bs + (bm + (n0 >> 4)) * sbytes, (last_b + 1) * sbytes);
+    const uint32_t gb = (uint32_t)gbytes, gs = (uint32_t)sbytes;
+    const uint32_t slot = MODE == kExpertRows ? (uint32_t)(m0 + lane) & 15u : (uint32_t)lane & 15u;
+    const bool next = MODE == kExpertRows && ((uint32_t)m0 & 15u) + ((uint32_t)lane & 15u) >= 16u;
+    // Tiles past the last one read it again (never multiplied), so that every
+    // step issues the same loads and the waits below are fixed counts.
+    const int n = (int)n_tiles;
+    auto issue = [&](int t, int stage) {
+        const int k = ((int)t0 + min(t, n - 1)) * kMxTileBytes;
 #pragma unroll
         for (int i = 0; i < T::LPW; ++i) {
             const int g = i * T::kWaves + wave;
-            __builtin_amdgcn_raw_ptr_buffer_load_lds(g < T::BM / 16 ? rA : rB, (lds_void_t*)(st + g * kMxTileBytes), 16,
-                                                     off[i], k, 0, 0);
+            const bool isa = i * T::kWaves < T::BM / 16;
+            const int last = isa ? last_a : last_b, grp = min(isa ? g : g - T::BM / 16, last);
+            uint32_t off = 16u * (uint32_t)lane;
+            if (MODE == kExpertRows && isa)
+                off = ((uint32_t)lane >> 4) * 256u + slot * 16u + (next && grp < last ? gb : 0u);
+            const int soff = (int)((uint32_t)grp * gb) + k;
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(isa ? rA : rB, (lds_void_t*)(smem + stage * T::kStage + g * kMxTileBytes),
+                                                     16, off, soff, 0, 0);
         }
     };
 
@@ -163,58 +164,79 @@ __global__ __launch_bounds__(T::kThreads, 2) void k_mx_gemm(MxGemmArgs p, int64_
     for (int i = 0; i < T::FM; ++i)
 #pragma unroll
         for (int j = 0; j < T::FN; ++j) acc[i][j] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
-    int sa[T::FM], sb[T::FN];
-    const int n = (int)n_tiles;
-
-    // one stage: publish it, refill the stage before it, multiply
-    auto step = [&](int t, auto STG) {
-        constexpr int stg = decltype(STG)::value;
-        const int later = min(T::STAGES - 2, n - 1 - t);   // younger tiles that may be in flight
-        if (later >= 2) wait_loads<2 * T::LPW>();
-        else if (later == 1) wait_loads<T::LPW>();
-        else wait_loads<0>();
+    // Operands of a stage in registers, two buffers: stage t + 1 is read while
+    // stage t is multiplied.  The scales of four tiles, one word a fragment,
+    // come straight from memory, two buffers too.
+    v4i fa[2][T::FM], fb[2][T::FN];
+    int sa[2][T::FM], sb[2][T::FN];
+    auto load_scales = [&](int unit, auto BUF) {
+        constexpr int buf = decltype(BUF)::value;
+        const int k = ((int)(t0 >> 2) + min(unit, (n - 1) >> 2)) * kMxUnitScales;
+#pragma unroll
+        for (int i = 0; i < T::FM; ++i) {
+            const int grp = min(wm * T::FM + i, last_a);
+            uint32_t off = 4u * (uint32_t)lane;
+            if (MODE == kExpertRows)
+                off = ((uint32_t)lane >> 4) * 64u + slot * 4u + (next && grp < last_a ? gs : 0u);
+            sa[buf][i] = (int)__builtin_amdgcn_raw_buffer_load_b32(rAs, off, (int)((uint32_t)grp * gs) + k, 0);
+        }
+#pragma unroll
+        for (int j = 0; j < T::FN; ++j)
+            sb[buf][j] = (int)__builtin_amdgcn_raw_buffer_load_b32(rBs, 4u * (uint32_t)lane,
+                                                                   (int)((uint32_t)min(wn * T::FN + j, last_b) * gs) + k, 0);
+    };
+    auto read_frags = [&](auto STG, auto BUF) {
+        constexpr int stg = decltype(STG)::value, buf = decltype(BUF)::value;
+        const uint8_t* st = smem + stg * T::kStage + 16 * lane;
+#pragma unroll
+        for (int i = 0; i < T::FM; ++i) fa[buf][i] = *reinterpret_cast<const v4i*>(st + (wm * T::FM + i) * kMxTileBytes);
+#pragma unroll
+        for (int j = 0; j < T::FN; ++j)
+            fb[buf][j] = *reinterpret_cast<const v4i*>(st + (T::BM / 16 + wn * T::FN + j) * kMxTileBytes);
+    };
+    // Step t, of index S in the cycle: publish stage t + 1, refill stage t's
+    // place (its operands were read in the step before), read stage t + 1's
+    // operands, multiply stage t's.
+    auto step = [&](int t, auto S) {
+        constexpr int s = decltype(S)::value, nxt = (s + 1) % T::STAGES, buf = s & 1, grp = (s >> 2) & 1;
+        wait_loads<(T::STAGES - 2) * T::LPW>();
         __builtin_amdgcn_s_barrier();
-        if (t + T::STAGES - 1 < n) issue(t + T::STAGES - 1);
-        if constexpr (stg == 0) {
-            const uint8_t* ss = smem + T::STAGES * T::kStage + ((t >> 2) & 1) * T::kScales + 4 * lane;
+        if constexpr ((s & 3) == 0) load_scales((t >> 2) + 1, std::integral_constant<int, grp ^ 1>());
+        issue(t + T::STAGES, s % T::STAGES);
+        read_frags(std::integral_constant<int, nxt>(), std::integral_constant<int, buf ^ 1>());
+#pragma unroll
+        for (int j = 0; j < T::FN; ++j)
 #pragma unroll
             for (int i = 0; i < T::FM; ++i)
-                sa[i] = *reinterpret_cast<const int*>(ss + (wm * T::FM + i) * kMxUnitScales);
+                acc[i][j] = mfma4<(s & 3)>(fb[buf][j], fa[buf][i], acc[i][j], sb[grp][j], sa[grp][i]);
+        constexpr int kReads = T::FM + T::FN, kMfma = T::FM * T::FN, kPer = kMfma / kReads > 0 ? kMfma / kReads : 1;
 #pragma unroll
-            for (int j = 0; j < T::FN; ++j)
-                sb[j] = *reinterpret_cast<const int*>(ss + (T::BM / 16 + wn * T::FN + j) * kMxUnitScales);
+        for (int g = 0; g < kReads; ++g) {
+            __builtin_amdgcn_sched_group_barrier(0x008, kPer, 0);   // MFMAs
+            __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);      // one LDS read
         }
-        const uint8_t* st = smem + stg * T::kStage + 16 * lane;
-        v4i fa[T::FM], fb[T::FN];
-#pragma unroll
-        for (int i = 0; i < T::FM; ++i) fa[i] = *reinterpret_cast<const v4i*>(st + (wm * T::FM + i) * kMxTileBytes);
-#pragma unroll
-        for (int j = 0; j < T::FN; ++j)
-            fb[j] = *reinterpret_cast<const v4i*>(st + (T::BM / 16 + wn * T::FN + j) * kMxTileBytes);
-#pragma unroll
-        for (int j = 0; j < T::FN; ++j)
-#pragma unroll
-            for (int i = 0; i < T::FM; ++i) acc[i][j] = mfma4<stg>(fb[j], fa[i], acc[i][j], sb[j], sa[i]);
     };
-    using I0 = std::integral_constant<int, 0>;
-    using I1 = std::integral_constant<int, 1>;
-    using I2 = std::integral_constant<int, 2>;
-    using I3 = std::integral_constant<int, 3>;
+    if (n > 0) {
+        load_scales(0, std::integral_constant<int, 0>());
 #pragma unroll
-    for (int s = 0; s < T::STAGES - 1; ++s)
-        if (s < n) issue(s);
-    for (int t = 0; t < n; t += 4) {
-        step(t, I0());
-        if (t + 1 < n) step(t + 1, I1());
-        if (t + 2 < n) step(t + 2, I2());
-        if (t + 3 < n) step(t + 3, I3());
+        for (int i = 0; i < T::STAGES; ++i) issue(i, i);
+        wait_loads<(T::STAGES - 1) * T::LPW>();
+        __builtin_amdgcn_s_barrier();
+        read_frags(std::integral_constant<int, 0>(), std::integral_constant<int, 0>());
+        for (int t = 0; t < n; t += T::kCycle)
+            unrolled_steps<T::kCycle>([&](auto S) {
+                constexpr int s = decltype(S)::value;
+                if (t + s >= n) return false;
+                step(t + s, S);
+                return true;
+            });
     }
 
     // ---- epilogue: 16 rows of a wave at a time through LDS, out in whole lines ----
     __builtin_amdgcn_s_waitcnt(0);
     __builtin_amdgcn_s_barrier();
     constexpr int kLd = T::TN + 4;
-    static_assert(T::kWaves * 16 * kLd * 4 <= T::kSmem, "a fragment row per wave fits");
+    static_assert(T::kWaves * 16 * kLd * 4 <= T::kSmem && 16 * (T::TN / 8) >= 64, "a fragment row per wave fits");
     float* tr = reinterpret_cast<float*>(smem) + wave * 16 * kLd;
     const int er = lane & 15, eq = lane >> 4;
     void* C = p.C;
@@ -238,7 +260,8 @@ __global__ __launch_bounds__(T::kThreads, 2) void k_mx_gemm(MxGemmArgs p, int64_
         constexpr int kPer = T::TN / 8, kRows = 64 / kPer;
         const int q = lane % kPer, r0 = lane / kPer;
 #pragma unroll
-        for (int r = r0; r < 16; r += kRows) {
+        for (int rr = 0; rr < 16; rr += kRows) {
+            const int r = r0 + rr;
             const float* src = tr + r * kLd + 8 * q;
             const v4f a = *reinterpret_cast<const v4f*>(src), b = *reinterpret_cast<const v4f*>(src + 4);
             const int64_t row = m + r, col = n_w + 8 * q, at = base + row * ldc + col;
@@ -377,7 +400,8 @@ hipError_t gemm_mode(const MxGemmArgs& a, hipStream_t s) {
     const int splits = (int)mx_gemm_splits(a);
     const double rows = MODE == kExpertRows ? (double)a.M / a.experts : (double)a.M;
     const double tiles = rows / 256.0 * ((double)a.N / 256.0) * (MODE == kDense ? 1.0 : (double)a.experts);
-    if (rows > 128 && a.N > 128 && tiles >= 192) return gemm<MxLarge, MODE>(a, splits, s);
+    if (!getenv("SQ_DUO") && rows > 128 && a.N > 128 && tiles >= 192) return gemm<MxLarge, MODE>(a, splits, s);
+    if (rows > 128 && a.N > 128 && tiles >= 192) return gemm<MxDuo, MODE>(a, splits, s);
     if (rows > 64 && a.N > 64 && tiles >= 24) return gemm<MxMid, MODE>(a, splits, s);
     return gemm<MxSmall, MODE>(a, splits, s);
 }
