@@ -773,8 +773,9 @@ sq_status sq_mx_gemm_experts_wgrad(const uint8_t* A, const uint8_t* A_scales, co
 /* ---------------------------------------------------------------------------
  * sq_mx_linear -- Y [M, N] = X W^T with X [M, K] in fp32 or bf16, quantized on the
  * way: what sq_mx_quantize and sq_mx_gemm (offsets NULL, experts 0) or
- * sq_mx_gemm_experts give.  Few rows (at most 16, or 16 an expert on average)
- * take one launch and no workspace, the serving form for single tokens.
+ * sq_mx_gemm_experts give.  Few rows (at most 16, or 16 an expert on average;
+ * more for small layers) take one launch and no workspace, the serving form
+ * for single tokens.
  * Workspace: sq_mx_linear_workspace_size bytes (0: none), 16-byte aligned.
  * Errors: as sq_mx_gemm.
  * ------------------------------------------------------------------------- */
@@ -784,6 +785,43 @@ sq_status sq_mx_linear(const void* X, int32_t type, int64_t M, int64_t K, int64_
                        const uint8_t* W, const uint8_t* W_scales, int64_t N,
                        void* Y, int32_t out_type, int64_t ldy,
                        void* workspace, size_t workspace_bytes, void* stream);
+
+/* ---------------------------------------------------------------------------
+ * sq_mx_layer -- the buffers of a linear layer that is trained, allocated once by
+ * the caller (host struct, read during the calls only), and its three steps:
+ *   sq_mx_layer_weight    codes of W [c_out, c_in] (a stack [experts] of such)
+ *                         along both axes, after each update of W
+ *   sq_mx_layer_forward   codes of X [rows, c_in] along both axes, Y = X W^T
+ *   sq_mx_layer_backward  codes of dY [rows, c_out] along both axes, then
+ *                         dX = dY W [rows, c_in] and dW = dY^T X [c_out, c_in]
+ *                         (a stack [experts] of such, ld_dw apart in its rows)
+ * Each is what sq_mx_quantize and the sq_mx_gemm calls give, in fewer launches:
+ * dX and dW share one.  Y and dX have the layer's type, dW is fp32.  offsets as
+ * above, NULL when experts == 0; the backward takes those of the forward, whose
+ * codes of X it reads.
+ * Sizes: w [c_out, c_in] and w_t [c_in, c_out], each experts times; x [rows, c_in],
+ * x_t [c_in, inner], dy [rows, c_out], dy_t [c_out, inner] with inner = rows, or
+ * sq_mx_segment_cols(rows, experts); every one of sq_mx_size bytes.
+ * Workspace: sq_mx_layer_workspace_size bytes (0: none), 16-byte aligned.
+ * Errors: as sq_mx_quantize and sq_mx_gemm.
+ * ------------------------------------------------------------------------- */
+typedef struct {
+    int64_t rows, c_in, c_out, experts;
+    int32_t type;                          /* SQ_TYPE_* of X, Y, dY, dX and W */
+    int32_t reserved;                      /* 0 */
+    uint8_t *w, *w_scales, *w_t, *w_t_scales;
+    uint8_t *x, *x_scales, *x_t, *x_t_scales;
+    uint8_t *dy, *dy_scales, *dy_t, *dy_t_scales;
+    void* workspace;
+    size_t workspace_bytes;
+} sq_mx_layer;
+
+sq_status sq_mx_layer_workspace_size(const sq_mx_layer* layer, size_t* bytes);
+sq_status sq_mx_layer_weight(const sq_mx_layer* layer, const void* W, int64_t ld, int64_t stride, void* stream);
+sq_status sq_mx_layer_forward(const sq_mx_layer* layer, const void* X, int64_t ld, const int32_t* offsets,
+                              void* Y, int64_t ldy, void* stream);
+sq_status sq_mx_layer_backward(const sq_mx_layer* layer, const void* dY, int64_t ld, const int32_t* offsets,
+                               void* dX, int64_t ld_dx, float* dW, int64_t ld_dw, void* stream);
 
 /* ---------------------------------------------------------------------------
  * sq_act_forward, sq_act_backward -- an activation between two layers, whose

@@ -14,25 +14,32 @@ namespace sq {
 
 namespace {
 
+// 8 consecutive elements as they came, 4 words of bf16 pairs or 8 of fp32;
+// columns at and past `cols` read as zero.
 template <typename T>
-__device__ __forceinline__ float value_of(T v) {
-    if constexpr (sizeof(T) == 4) return v;
-    else return bf16_value(v);
-}
-
-// 8 consecutive elements; columns at and past `cols` read as zero.
-template <typename T>
-__device__ __forceinline__ void load8(const T* row, int64_t c, int64_t cols, bool vec, float* f) {
+__device__ __forceinline__ void load8(const T* row, int64_t c, int64_t cols, bool vec, uint32_t* w) {
     if (vec && c + 8 <= cols) {
+#pragma unroll
+        for (int i = 0; i < (int)(8 * sizeof(T) / 4); i += 4) {
+            const uint4 v = *reinterpret_cast<const uint4*>(row + c + i * 4 / sizeof(T));
+            w[i] = v.x;
+            w[i + 1] = v.y;
+            w[i + 2] = v.z;
+            w[i + 3] = v.w;
+        }
+    } else {
         T v[8];
 #pragma unroll
-        for (int w = 0; w < (int)(8 * sizeof(T) / 16); ++w)
-            reinterpret_cast<uint4*>(v)[w] = reinterpret_cast<const uint4*>(row + c)[w];
+        for (int e = 0; e < 8; ++e) v[e] = c + e < cols ? row[c + e] : (T)0;
+        __builtin_memcpy(w, v, sizeof(v));
+    }
+}
+template <typename T>
+__device__ __forceinline__ void values8(const uint32_t* w, float* f) {
 #pragma unroll
-        for (int e = 0; e < 8; ++e) f[e] = value_of<T>(v[e]);
-    } else {
-#pragma unroll
-        for (int e = 0; e < 8; ++e) f[e] = c + e < cols ? value_of<T>(row[c + e]) : 0.0f;
+    for (int e = 0; e < 8; ++e) {
+        if constexpr (sizeof(T) == 4) f[e] = __uint_as_float(w[e]);
+        else f[e] = __uint_as_float(e & 1 ? w[e >> 1] & 0xFFFF0000u : w[e >> 1] << 16);
     }
 }
 
@@ -73,19 +80,34 @@ __device__ __forceinline__ float gate(float x, float& slope) {
 }
 
 // The 8-bit copy of 8 elements; four lanes hold a block of 32.
-__device__ __forceinline__ void copy8(const float* f, int8_t* codes, uint8_t* scale, bool first) {
+template <typename T>
+__device__ __forceinline__ void copy8(const uint32_t* raw, const float* f, int8_t* codes, uint8_t* scale, bool first) {
     uint32_t b = 0;
+    if constexpr (sizeof(T) == 4) {
 #pragma unroll
-    for (int e = 0; e < 8; ++e) b = max(b, __float_as_uint(f[e]) & 0x7FFFFFFFu);
+        for (int e = 0; e < 8; ++e) b = max(b, raw[e] & 0x7FFFFFFFu);
+    } else {
+        typedef uint16_t v2u16 __attribute__((ext_vector_type(2)));
+        v2u16 m = {0, 0};
+#pragma unroll
+        for (int e = 0; e < 4; ++e) m = __builtin_elementwise_max(m, __builtin_bit_cast(v2u16, raw[e] & 0x7FFF7FFFu));
+        b = (uint32_t)max(m.x, m.y) << 16;
+    }
     b = max(b, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)b, 0xB1, 0xF, 0xF, false));   // lane ^ 1
     b = max(b, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)b, 0x4E, 0xF, 0xF, false));   // lane ^ 2
     const uint32_t s = mx_scale8(b);
     const float inv = mx_inverse(s);
-    uint32_t w[2] = {0u, 0u};
+    // x inv is exact (a power of two), so 1.5 2^23 + x inv rounds once, to the
+    // nearest even integer, which its low byte holds in two's complement
+    uint32_t k[8];
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-        const int k = s == 255u ? 0 : (int)__builtin_rintf(f[e] * inv);
-        w[e >> 2] |= ((uint32_t)k & 255u) << (8 * (e & 3));
+    for (int e = 0; e < 8; ++e) k[e] = __float_as_uint(__builtin_fmaf(f[e], inv, 12582912.0f));
+    uint32_t w[2];
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        const uint32_t lo = __builtin_amdgcn_perm(k[4 * h + 1], k[4 * h], 0x0C0C0400u);
+        const uint32_t hi = __builtin_amdgcn_perm(k[4 * h + 3], k[4 * h + 2], 0x04000C0Cu);
+        w[h] = s == 255u ? 0u : lo | hi;
     }
     *reinterpret_cast<uint2*>(codes) = make_uint2(w[0], w[1]);
     if (first) *scale = (uint8_t)s;
@@ -97,43 +119,64 @@ __device__ __forceinline__ void from_copy8(const int8_t* codes, const uint8_t* s
     for (int e = 0; e < 8; ++e) f[e] = (float)(int8_t)((e < 4 ? w.x : w.y) >> (8 * (e & 3))) * s;
 }
 
+// Row and column of a thread: item / chunks by a multiplication, exact for
+// items below 2^31 (mul = ceil(2^(31 + shift) / chunks), 2^shift >= chunks).
+struct ActGrid {
+    uint32_t items, chunks, mul;
+    int shift;
+    bool vec;
+};
+__device__ __forceinline__ uint32_t row_of(const ActGrid& g, uint32_t i) {
+    return (uint32_t)(((uint64_t)i * g.mul) >> (31 + g.shift));
+}
+
 // A thread takes 8 columns of a row of the padded width Fp = roundup(F, 32).
 template <typename T, int KIND, bool GATED>
-__global__ __launch_bounds__(256) void k_act_forward(ActArgs p, int64_t n, uint32_t chunks, bool vec) {
-    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
-    if (i >= n) return;
-    const int64_t r = i / chunks, c = (i - r * chunks) * 8, fp = (int64_t)chunks * 8;
+__global__ __launch_bounds__(256) void k_act_forward(ActArgs p, ActGrid q) {
+    const uint32_t i = blockIdx.x * 256u + threadIdx.x;
+    if (i >= q.items) return;
+    const uint32_t row = row_of(q, i);
+    const int64_t r = row, c = (int64_t)(i - row * q.chunks) * 8, fp = (int64_t)q.chunks * 8;
     const int64_t ldc = GATED ? 2 * fp : fp;
     const T* x = static_cast<const T*>(p.x) + r * p.ld_x;
     int8_t* codes = p.codes + r * ldc;
     uint8_t* scales = p.scales + r * (ldc / 32);
+    constexpr int kWords = 8 * sizeof(T) / 4;
+    uint32_t gw[kWords], uw[kWords];
     float g[8], u[8], h[8];
-    load8<T>(x, c, p.F, vec, g);
-    if constexpr (GATED) load8<T>(x + p.F, c, p.F, vec, u);
+    load8<T>(x, c, p.F, q.vec, gw);
+    if constexpr (GATED) load8<T>(x + p.F, c, p.F, q.vec, uw);
     const bool first = (threadIdx.x & 3) == 0;
-    copy8(g, codes + c, scales + (c >> 5), first);
-    if constexpr (GATED) copy8(u, codes + fp + c, scales + ((fp + c) >> 5), first);
+    values8<T>(gw, g);
+    copy8<T>(gw, g, codes + c, scales + (c >> 5), first);
+    if constexpr (GATED) {
+        values8<T>(uw, u);
+        copy8<T>(uw, u, codes + fp + c, scales + ((fp + c) >> 5), first);
+    }
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
         float slope;
         h[e] = g[e] * gate<KIND>(g[e], slope);
         if constexpr (GATED) h[e] *= u[e];
     }
-    store8<T>(static_cast<T*>(p.h) + r * p.ld_h, c, p.F, vec, h);
+    store8<T>(static_cast<T*>(p.h) + r * p.ld_h, c, p.F, q.vec, h);
 }
 
 template <typename T, int KIND, bool GATED>
-__global__ __launch_bounds__(256) void k_act_backward(ActArgs p, int64_t n, uint32_t chunks, bool vec) {
-    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
-    if (i >= n) return;
-    const int64_t r = i / chunks, c = (i - r * chunks) * 8, fp = (int64_t)chunks * 8;
+__global__ __launch_bounds__(256) void k_act_backward(ActArgs p, ActGrid q) {
+    const uint32_t i = blockIdx.x * 256u + threadIdx.x;
+    if (i >= q.items) return;
+    const uint32_t row = row_of(q, i);
+    const int64_t r = row, c = (int64_t)(i - row * q.chunks) * 8, fp = (int64_t)q.chunks * 8;
     const int64_t ldc = GATED ? 2 * fp : fp;
     const int8_t* codes = p.codes + r * ldc;
     const uint8_t* scales = p.scales + r * (ldc / 32);
+    uint32_t dw[8 * sizeof(T) / 4];
     float g[8], u[8], d[8];
-    load8<T>(static_cast<const T*>(p.h) + r * p.ld_h, c, p.F, vec, d);
+    load8<T>(static_cast<const T*>(p.h) + r * p.ld_h, c, p.F, q.vec, dw);
     from_copy8(codes + c, scales + (c >> 5), g);
     if constexpr (GATED) from_copy8(codes + fp + c, scales + ((fp + c) >> 5), u);
+    values8<T>(dw, d);
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
         float slope;
@@ -147,19 +190,36 @@ __global__ __launch_bounds__(256) void k_act_backward(ActArgs p, int64_t n, uint
         }
     }
     T* dx = static_cast<T*>(p.dx) + r * p.ld_x;
-    store8<T>(dx, c, p.F, vec, g);
-    if constexpr (GATED) store8<T>(dx + p.F, c, p.F, vec, u);
+    store8<T>(dx, c, p.F, q.vec, g);
+    if constexpr (GATED) store8<T>(dx + p.F, c, p.F, q.vec, u);
 }
 
 template <typename T, int KIND, bool GATED>
-hipError_t act(const ActArgs& a, bool forward, hipStream_t s) {
-    const int64_t chunks = round_up(a.F, 32) / 8, n = a.M * chunks;
+hipError_t act(const ActArgs& args, bool forward, hipStream_t s) {
+    ActArgs a = args;
+    const int64_t chunks = round_up(a.F, 32) / 8, fp = chunks * 8, codes_ld = GATED ? 2 * fp : fp;
     auto ok = [](const void* p, int64_t ld) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0 && (ld * sizeof(T)) % 16 == 0; };
-    const bool vec = ok(forward ? a.x : a.dx, a.ld_x) && ok(a.h, a.ld_h) && (!GATED || (a.F * sizeof(T)) % 16 == 0);
-    const uint32_t blocks = (uint32_t)((n + 255) / 256);
-    if (forward) k_act_forward<T, KIND, GATED><<<blocks, 256, 0, s>>>(a, n, (uint32_t)chunks, vec);
-    else k_act_backward<T, KIND, GATED><<<blocks, 256, 0, s>>>(a, n, (uint32_t)chunks, vec);
-    return hipGetLastError();
+    ActGrid q{};
+    q.vec = ok(forward ? a.x : a.dx, a.ld_x) && ok(a.h, a.ld_h) && (!GATED || (a.F * sizeof(T)) % 16 == 0);
+    q.chunks = (uint32_t)chunks;
+    while (((int64_t)1 << q.shift) < chunks) ++q.shift;
+    q.mul = (uint32_t)((((uint64_t)1 << (31 + q.shift)) + (uint64_t)chunks - 1) / (uint64_t)chunks);
+    // as many rows a launch as keep its items below 2^31
+    const int64_t most = (((int64_t)1 << 31) - 256) / chunks;
+    for (int64_t left = args.M; left > 0; left -= most) {
+        q.items = (uint32_t)(std::min(left, most) * chunks);
+        const uint32_t blocks = (q.items + 255) / 256;
+        if (forward) k_act_forward<T, KIND, GATED><<<blocks, 256, 0, s>>>(a, q);
+        else k_act_backward<T, KIND, GATED><<<blocks, 256, 0, s>>>(a, q);
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess) return e;
+        a.x = a.x ? static_cast<const T*>(a.x) + most * a.ld_x : nullptr;
+        a.dx = a.dx ? static_cast<T*>(a.dx) + most * a.ld_x : nullptr;
+        a.h = static_cast<T*>(a.h) + most * a.ld_h;
+        a.codes += most * codes_ld;
+        a.scales += most * (codes_ld / 32);
+    }
+    return hipSuccess;
 }
 
 template <typename T>

@@ -68,9 +68,13 @@ struct MxGemmArgs {
     int type;
     int64_t ldc;                           // kExpertInner: matrix e at e * M * ldc
     float* part;                           // split-K partials [splits, M, N] (kDense)
+    bool stream_out;                       // fp32 C past the caches: a weight gradient, which the optimizer reads later
 };
 int64_t mx_gemm_splits(const MxGemmArgs& a);      // K splits of the product (1 unless kDense)
 hipError_t launch_mx_gemm(const MxGemmArgs& a, hipStream_t s);
+// Both products, one launch where they take the same tiles: two of kDense, or
+// kExpertRows and kExpertInner.  Their K splits' partials must not overlap.
+hipError_t launch_mx_gemm_pair(const MxGemmArgs& a, const MxGemmArgs& b, hipStream_t s);
 
 // Few rows: Y = X W^T with the rows of X quantized on the way.
 struct MxRowsArgs {
@@ -85,7 +89,7 @@ struct MxRowsArgs {
     int out_type;
     int64_t ldy;
 };
-bool mx_rows_ok(int64_t M, int64_t K, int64_t N, int64_t experts);
+bool mx_rows_ok(int64_t M, int64_t K, int64_t N, int64_t experts, int type);
 hipError_t launch_mx_rows(const MxRowsArgs& a, hipStream_t s);
 
 // ---- activations (sq_act.hip) ----
@@ -139,12 +143,15 @@ __device__ __forceinline__ void segment_of(const int32_t* offsets, int experts, 
         hi = min(max(offsets[e + 1], lo), rows);
     }
 }
-__device__ __forceinline__ int wave_scan(int v, int lane) {   // inclusive
-#pragma unroll
-    for (int d = 1; d < 64; d <<= 1) {
-        const int o = __shfl_up(v, d);
-        if (lane >= d) v += o;
-    }
+// Inclusive sum over the lanes of a wave: within rows of 16 lanes by shifts,
+// then the row totals broadcast onward.  Every lane must be active.
+__device__ __forceinline__ int wave_scan(int v) {
+    v += __builtin_amdgcn_update_dpp(0, v, 0x111, 0xF, 0xF, false);   // row_shr:1
+    v += __builtin_amdgcn_update_dpp(0, v, 0x112, 0xF, 0xF, false);   // row_shr:2
+    v += __builtin_amdgcn_update_dpp(0, v, 0x114, 0xF, 0xF, false);   // row_shr:4
+    v += __builtin_amdgcn_update_dpp(0, v, 0x118, 0xF, 0xF, false);   // row_shr:8
+    v += __builtin_amdgcn_update_dpp(0, v, 0x142, 0xA, 0xF, false);   // row_bcast:15 into rows 1 and 3
+    v += __builtin_amdgcn_update_dpp(0, v, 0x143, 0xC, 0xF, false);   // row_bcast:31 into rows 2 and 3
     return v;
 }
 __device__ __forceinline__ Segment find_segment(const int32_t* offsets, int experts, int rows, int unit, int index) {
@@ -156,7 +163,7 @@ __device__ __forceinline__ Segment find_segment(const int32_t* offsets, int expe
         int lo, hi;
         segment_of(offsets, experts, rows, base + lane, lo, hi);
         const int t = (hi - lo + unit - 1) / unit, k = (hi - lo + kMxUnit - 1) / kMxUnit;
-        const int ti = wave_scan(t, lane), ki = wave_scan(k, lane);
+        const int ti = wave_scan(t), ki = wave_scan(k);
         const uint64_t hit = __ballot(index >= tiles + ti - t && index < tiles + ti);
         if (hit) {
             const int src = __ffsll((unsigned long long)hit) - 1;
@@ -181,7 +188,7 @@ __device__ __forceinline__ void segment_inner(const int32_t* offsets, int expert
     for (int base = 0; base < experts; base += 64) {
         int lo, hi;
         segment_of(offsets, experts, rows, base + lane, lo, hi);
-        const int k = (hi - lo + kMxUnit - 1) / kMxUnit, ki = wave_scan(k, lane);
+        const int k = (hi - lo + kMxUnit - 1) / kMxUnit, ki = wave_scan(k);
         if (e < base + 64) {
             inner += (int64_t)__builtin_amdgcn_readlane(ki - k, e - base) * kMxUnit;
             len = __builtin_amdgcn_readlane(hi - lo, e - base);
@@ -193,13 +200,12 @@ __device__ __forceinline__ void segment_inner(const int32_t* offsets, int expert
 
 __device__ __forceinline__ float bf16_value(uint32_t b) { return __uint_as_float(b << 16); }
 // round to nearest even; NaN stays NaN
-__device__ __forceinline__ uint32_t bf16_bits(float v) {
-    const __bf16 b = (__bf16)v;
-    uint16_t u;
-    __builtin_memcpy(&u, &b, 2);
-    return u;
+__device__ __forceinline__ uint32_t bf16_pair(float a, float b) {
+    typedef float v2f __attribute__((ext_vector_type(2)));
+    typedef __bf16 v2b __attribute__((ext_vector_type(2)));
+    return __builtin_bit_cast(uint32_t, __builtin_convertvector(v2f{a, b}, v2b));
 }
-__device__ __forceinline__ uint32_t bf16_pair(float a, float b) { return bf16_bits(a) | bf16_bits(b) << 16; }
+__device__ __forceinline__ uint32_t bf16_bits(float v) { return bf16_pair(v, 0.0f) & 0xFFFFu; }
 #endif
 
 }  // namespace sq

@@ -93,15 +93,16 @@ struct QuantTile<uint16_t> {   // bf16 bits
 // vector instructions bound the kernel, not HBM, when each element was
 // unpacked and multiplied by the scale's inverse (8192 x 11008 both ways 84 us).
 template <typename T>
-__global__ __launch_bounds__(256) void k_mx_quantize(MxQuantArgs p, int64_t tiles_c, bool vec) {
+__global__ __launch_bounds__(256) void k_mx_quantize(MxQuantArgs p, uint32_t tiles_c, bool vec) {
     constexpr int TC = QuantTile<T>::TC, kLanes = TC / 8, kPass = 64 / kLanes, kPasses = 32 / kPass;
     constexpr int kWords = 8 * sizeof(T) / 4;            // words a lane loads of a row
     constexpr int kCols = 4 / sizeof(T);                 // columns a lane takes of the transpose
     __shared__ __attribute__((aligned(16))) uint32_t tile[128][TC * sizeof(T) / 4];
 
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    const int64_t tr = blockIdx.x / tiles_c, tc = blockIdx.x - tr * tiles_c, mat = blockIdx.y;
-    int64_t row0 = tr * 128, row_end = p.rows, inner = row0;
+    const uint32_t tr = blockIdx.x / tiles_c, tc = blockIdx.x - tr * tiles_c;
+    const int64_t mat = blockIdx.y;
+    int64_t row0 = (int64_t)tr * 128, row_end = p.rows, inner = row0;
     if (p.offsets) {
         const Segment g = find_segment(p.offsets, p.experts, (int)p.rows, 128, (int)tr);
         if (g.expert < 0) return;
@@ -109,7 +110,7 @@ __global__ __launch_bounds__(256) void k_mx_quantize(MxQuantArgs p, int64_t tile
         row_end = g.hi;
         inner = g.inner + (int64_t)g.tile * 128;
     }
-    const int64_t col0 = tc * TC;
+    const int64_t col0 = (int64_t)tc * TC;
     const T* x = static_cast<const T*>(p.x) + mat * p.stride;
 
     const int q = lane % kLanes, r0 = wave * 32 + lane / kLanes;
@@ -257,7 +258,7 @@ hipError_t quantize(const MxQuantArgs& a, hipStream_t s) {
     const int64_t tiles_r = a.offsets ? a.rows / 128 + std::min<int64_t>(a.experts, a.rows) : (a.rows + 127) / 128;
     const bool vec = (reinterpret_cast<uintptr_t>(a.x) & 15) == 0 && (a.ld * sizeof(T)) % 16 == 0 &&
                      (a.batch == 1 || (a.stride * sizeof(T)) % 16 == 0);
-    k_mx_quantize<T><<<dim3((uint32_t)(tiles_r * tiles_c), (uint32_t)a.batch), 256, 0, s>>>(a, tiles_c, vec);
+    k_mx_quantize<T><<<dim3((uint32_t)(tiles_r * tiles_c), (uint32_t)a.batch), 256, 0, s>>>(a, (uint32_t)tiles_c, vec);
     return hipGetLastError();
 }
 

@@ -97,9 +97,9 @@ struct LinearWorkspace {
     size_t codes = 0, scales = 0, part = 0;
     size_t bytes() const { return codes + scales + part; }
 };
-LinearWorkspace linear_workspace(int64_t M, int64_t K, int64_t N, int64_t experts) {
+LinearWorkspace linear_workspace(int64_t M, int64_t K, int64_t N, int64_t experts, int type) {
     LinearWorkspace w;
-    if (M == 0 || N == 0 || mx_rows_ok(M, K, N, experts)) return w;
+    if (M == 0 || N == 0 || mx_rows_ok(M, K, N, experts, type)) return w;
     w.codes = (size_t)round_up(mx_code_bytes(M, K), 256);
     w.scales = (size_t)round_up(mx_scale_bytes(M, K), 256);
     MxGemmArgs a{};
@@ -314,6 +314,7 @@ sq_status sq_mx_gemm_experts_wgrad(const uint8_t* A, const uint8_t* A_scales, co
         a.C = C;
         a.type = type;
         a.ldc = ldc;
+        a.stream_out = true;
         return hip_status(launch_mx_gemm(a, static_cast<hipStream_t>(stream)), "mx weight gradient by expert");
     });
 }
@@ -323,7 +324,8 @@ sq_status sq_mx_linear_workspace_size(int64_t M, int64_t K, int64_t N, int64_t e
         if (experts < 0 || experts >= kMaxExperts) return invalid("experts is out of range");
         SQ_TRY(check_product(M, N, K, experts));
         if (!bytes) return invalid("bytes is NULL");
-        *bytes = linear_workspace(M, K, N, experts).bytes();
+        *bytes = std::max(linear_workspace(M, K, N, experts, SQ_TYPE_F32).bytes(),
+                          linear_workspace(M, K, N, experts, SQ_TYPE_BF16).bytes());
         return SQ_OK;
     });
 }
@@ -343,10 +345,10 @@ sq_status sq_mx_linear(const void* X, int32_t type, int64_t M, int64_t K, int64_
             SQ_TRY(check_mx(W, W_scales, "W"));
         }
         SQ_TRY(check_values(Y, out_type, ldy, N, "Y"));
-        const LinearWorkspace w = linear_workspace(M, K, N, experts);
+        const LinearWorkspace w = linear_workspace(M, K, N, experts, type);
         SQ_TRY(check_workspace(workspace, workspace_bytes, w.bytes()));
         hipStream_t s = static_cast<hipStream_t>(stream);
-        if (mx_rows_ok(M, K, N, experts)) {
+        if (mx_rows_ok(M, K, N, experts, type)) {
             MxRowsArgs r{};
             r.x = X;
             r.type = type;
@@ -369,6 +371,126 @@ sq_status sq_mx_linear(const void* X, int32_t type, int64_t M, int64_t K, int64_
         if (experts)
             return sq_mx_gemm_experts(codes, scales, M, K, offsets, experts, W, W_scales, N, Y, out_type, ldy, stream);
         return sq_mx_gemm(codes, scales, W, W_scales, M, N, K, Y, out_type, ldy, scales + w.scales, w.part, stream);
+    });
+}
+
+// ---------------------------------------------------------------------------
+static sq_status check_layer(const sq_mx_layer* l) {
+    if (!l) return invalid("layer is NULL");
+    SQ_TRY(check_type(l->type));
+    if (l->experts < 0 || l->experts >= kMaxExperts) return invalid("experts is out of range");
+    SQ_TRY(check_dim(l->rows, kMaxRows, "rows"));
+    SQ_TRY(check_dim(l->c_in, kMaxCols, "c_in"));
+    SQ_TRY(check_dim(l->c_out, kMaxCols, "c_out"));
+    return check_inner(l->rows);
+}
+
+static sq_status check_layer_offsets(const sq_mx_layer* l, const int32_t* offsets) {
+    if (l->experts) return check_experts(offsets, l->experts);
+    if (offsets) return invalid("offsets without experts");
+    return SQ_OK;
+}
+
+// the products dX [rows, c_in] = dY W and dW [c_out, c_in] = dY^T X, their K splits' partials one after the other
+static void backward_args(const sq_mx_layer* l, MxGemmArgs& x, MxGemmArgs& w) {
+    x = dense_args(l->rows, l->c_in, l->c_out);
+    x.mode = l->experts ? kExpertRows : kDense;
+    x.experts = (int)l->experts;
+    w = dense_args(l->c_out, l->c_in, l->experts ? mx_segment_cols(l->rows, l->experts) : l->rows);
+    w.mode = l->experts ? kExpertInner : kDense;
+    w.experts = (int)l->experts;
+    w.rows = l->rows;
+    w.stream_out = true;
+}
+
+static size_t layer_workspace(const sq_mx_layer* l) {
+    if (l->experts || l->c_in == 0 || l->c_out == 0) return 0;
+    MxGemmArgs x, w;
+    backward_args(l, x, w);
+    return std::max(l->rows ? part_bytes(dense_args(l->rows, l->c_out, l->c_in)) : 0,
+                    (l->rows ? part_bytes(x) : 0) + part_bytes(w));
+}
+
+sq_status sq_mx_layer_workspace_size(const sq_mx_layer* layer, size_t* bytes) {
+    return guarded([&]() -> sq_status {
+        SQ_TRY(check_layer(layer));
+        if (!bytes) return invalid("bytes is NULL");
+        *bytes = layer_workspace(layer);
+        return SQ_OK;
+    });
+}
+
+sq_status sq_mx_layer_weight(const sq_mx_layer* layer, const void* W, int64_t ld, int64_t stride, void* stream) {
+    return guarded([&]() -> sq_status {
+        SQ_TRY(check_layer(layer));
+        const sq_mx_layer& l = *layer;
+        return sq_mx_quantize(W, l.type, l.experts ? l.experts : 1, l.c_out, l.c_in, ld, stride, nullptr, 0, l.w, l.w_scales,
+                              l.w_t, l.w_t_scales, stream);
+    });
+}
+
+sq_status sq_mx_layer_forward(const sq_mx_layer* layer, const void* X, int64_t ld, const int32_t* offsets, void* Y, int64_t ldy,
+                              void* stream) {
+    return guarded([&]() -> sq_status {
+        SQ_TRY(check_layer(layer));
+        const sq_mx_layer& l = *layer;
+        SQ_TRY(check_layer_offsets(layer, offsets));
+        SQ_TRY(check_product(l.rows, l.c_out, l.c_in, l.experts));
+        if (l.rows > 0 && l.c_out > 0) {
+            SQ_TRY(check_values(Y, l.type, ldy, l.c_out, "Y"));
+            if (l.c_in > 0) SQ_TRY(check_mx(l.w, l.w_scales, "w"));
+        }
+        SQ_TRY(check_workspace(l.workspace, l.workspace_bytes, layer_workspace(layer)));
+        SQ_TRY(sq_mx_quantize(X, l.type, 1, l.rows, l.c_in, ld, 0, offsets, l.experts, l.x, l.x_scales, l.x_t, l.x_t_scales,
+                              stream));
+        if (l.experts)
+            return sq_mx_gemm_experts(l.x, l.x_scales, l.rows, l.c_in, offsets, l.experts, l.w, l.w_scales, l.c_out, Y, l.type,
+                                      ldy, stream);
+        return sq_mx_gemm(l.x, l.x_scales, l.w, l.w_scales, l.rows, l.c_out, l.c_in, Y, l.type, ldy, l.workspace,
+                          l.workspace_bytes, stream);
+    });
+}
+
+sq_status sq_mx_layer_backward(const sq_mx_layer* layer, const void* dY, int64_t ld, const int32_t* offsets, void* dX,
+                               int64_t ld_dx, float* dW, int64_t ld_dw, void* stream) {
+    return guarded([&]() -> sq_status {
+        SQ_TRY(check_layer(layer));
+        const sq_mx_layer& l = *layer;
+        SQ_TRY(check_layer_offsets(layer, offsets));
+        SQ_TRY(check_product(l.rows, l.c_in, l.c_out, l.experts));
+        SQ_TRY(check_blocks(l.c_out, 16, l.c_in, 16, 0, std::max<int64_t>(l.experts, 1)));
+        if (l.rows > 0 && l.c_in > 0) {
+            SQ_TRY(check_values(dX, l.type, ld_dx, l.c_in, "dX"));
+            if (l.c_out > 0) SQ_TRY(check_mx(l.w_t, l.w_t_scales, "w_t"));
+        }
+        if (l.c_out > 0 && l.c_in > 0) {
+            SQ_TRY(check_values(dW, SQ_TYPE_F32, ld_dw, l.c_in, "dW"));
+            if (l.rows > 0) SQ_TRY(check_mx(l.x_t, l.x_t_scales, "x_t"));
+        }
+        SQ_TRY(check_workspace(l.workspace, l.workspace_bytes, layer_workspace(layer)));
+        SQ_TRY(sq_mx_quantize(dY, l.type, 1, l.rows, l.c_out, ld, 0, offsets, l.experts, l.dy, l.dy_scales, l.dy_t,
+                              l.dy_t_scales, stream));
+        MxGemmArgs x, w;
+        backward_args(layer, x, w);
+        x.A = l.dy;
+        x.As = l.dy_scales;
+        x.B = l.w_t;
+        x.Bs = l.w_t_scales;
+        x.offsets = offsets;
+        x.C = dX;
+        x.type = l.type;
+        x.ldc = ld_dx;
+        x.part = static_cast<float*>(l.workspace);
+        w.A = l.dy_t;
+        w.As = l.dy_t_scales;
+        w.B = l.x_t;
+        w.Bs = l.x_t_scales;
+        w.offsets = offsets;
+        w.C = dW;
+        w.type = SQ_TYPE_F32;
+        w.ldc = ld_dw;
+        w.part = x.part + (l.experts || l.rows == 0 ? 0 : part_bytes(x) / sizeof(float));
+        return hip_status(launch_mx_gemm_pair(x, w, static_cast<hipStream_t>(stream)), "mx gradients");
     });
 }
 

@@ -185,6 +185,41 @@ def sq_mx_linear(X, W, W_scales, Y, workspace=None, offsets=None, experts=0, str
         _type(Y), _rows(Y, "Y"), ws, nws, _stream(stream)))
 
 
+class Layer(ct.Structure):
+    """sq_mx_layer"""
+    _fields_ = ([(n, _I64) for n in ("rows", "c_in", "c_out", "experts")] + [("type", ct.c_int32), ("reserved", ct.c_int32)]
+                + [(m + s, ct.c_void_p) for m in ("w", "w_t", "x", "x_t", "dy", "dy_t") for s in ("", "_scales")]
+                + [("workspace", ct.c_void_p), ("workspace_bytes", _SZ)])
+
+
+def sq_mx_layer_workspace_size(layer: Layer) -> int:
+    nb = _SZ(0)
+    _check("sq_mx_layer_workspace_size", load().sq_mx_layer_workspace_size(ct.addressof(layer), ct.byref(nb)))
+    return nb.value
+
+
+def sq_mx_layer_weight(layer: Layer, W, stream=None) -> None:
+    """W [c_out, c_in], or [experts, c_out, c_in]"""
+    st = W.stride()
+    if st[-1] != 1 and W.shape[-1] > 1:
+        raise ValueError("W: expected unit column stride")
+    ld = st[-2] if W.shape[-2] > 1 else max(st[-2], W.shape[-1])
+    _check("sq_mx_layer_weight", load().sq_mx_layer_weight(ct.addressof(layer), W.data_ptr(), ld, st[0], _stream(stream)))
+
+
+def sq_mx_layer_forward(layer: Layer, X, offsets, Y, stream=None) -> None:
+    _check("sq_mx_layer_forward", load().sq_mx_layer_forward(
+        ct.addressof(layer), X.data_ptr(), _rows(X, "X"), None if offsets is None else offsets.data_ptr(), Y.data_ptr(),
+        _rows(Y, "Y"), _stream(stream)))
+
+
+def sq_mx_layer_backward(layer: Layer, dY, offsets, dX, dW, stream=None) -> None:
+    """dW [c_out, c_in] or [experts, c_out, c_in], contiguous"""
+    _check("sq_mx_layer_backward", load().sq_mx_layer_backward(
+        ct.addressof(layer), dY.data_ptr(), _rows(dY, "dY"), None if offsets is None else offsets.data_ptr(), dX.data_ptr(),
+        _rows(dX, "dX"), dW.data_ptr(), max(dW.shape[-1], 1), _stream(stream)))
+
+
 def sq_act_size(M: int, F: int, gated: bool) -> Tuple[int, int]:
     a, b = _SZ(0), _SZ(0)
     _check("sq_act_size", load().sq_act_size(M, F, int(gated), ct.byref(a), ct.byref(b)))
@@ -226,6 +261,24 @@ def quantize(X: torch.Tensor, rows: bool = True, cols: bool = False, offsets: Op
     return a, t
 
 
+# The plans' calls run once per launch or two, so their own time bounds small
+# layers (a token through 4096 x 4096: 6.4 us a call through the wrappers above,
+# 4.5 us on the GPU): an input is looked at once, and what does not change from
+# call to call is kept as integers.
+def _checked(t: torch.Tensor, shape, dtype, name: str) -> int:
+    """The row stride of a plan's input, after a look at its shape, type, place and strides."""
+    if t.shape != shape:
+        raise ValueError(f"{name}: expected shape {tuple(shape)}, got {tuple(t.shape)}")
+    if t.dtype is not dtype:
+        raise TypeError(f"{name}: expected {dtype}, got {t.dtype}")
+    if not t.is_cuda:
+        raise ValueError(f"{name}: expected a tensor on the GPU")
+    st = t.stride()
+    if st[-1] != 1 and shape[-1] > 1:
+        raise ValueError(f"{name}: expected unit column stride")
+    return st[-2] if shape[-2] > 1 else max(st[-2], shape[-1])
+
+
 class LinearPlan:
     """A linear layer Y = X W^T on M rows with microscaled 4-bit operands, all of
     its buffers allocated once.  ``experts`` > 0: that many weight matrices; the
@@ -244,65 +297,76 @@ class LinearPlan:
             raise TypeError(f"dtype: expected float32 or bfloat16, got {dtype}")
         dev = torch.device(device)
         self.M, self.C_in, self.C_out, self.dtype, self.experts, self.train = M, C_in, C_out, dtype, experts, train
-        self.Y = torch.empty((M, C_out), dtype=dtype, device=dev)
-        self.offsets = None
+        self._x_shape, self._y_shape = torch.Size((M, C_in)), torch.Size((M, C_out))
+        self._w_shape = torch.Size((experts, C_out, C_in) if experts else (C_out, C_in))
+        self.Y = torch.empty(self._y_shape, dtype=dtype, device=dev)
+        self.offsets, self._off_ptr, self._type = None, None, _TYPES[dtype]
+        self._y_ptr, self._y_ld, self._lib = self.Y.data_ptr(), max(C_out, 1), load()
         if not train:
             self.ws = _workspace(sq_mx_linear_workspace_size(M, C_in, C_out, experts), dev)
+            self._ws = _ws_ptr(self.ws)
+            self._held = [self.Y, self.ws]      # the pointers kept stay valid as long as the plan
             return
         inner = sq_mx_segment_cols(M, experts) if experts else M
         self.w = MxMatrix.empty(C_out, C_in, experts, dev)
         self.w_t = MxMatrix.empty(C_in, C_out, experts, dev)
         self.x, self.x_t = MxMatrix.empty(M, C_in, 0, dev), MxMatrix.empty(C_in, inner, 0, dev)
         self.dy, self.dy_t = MxMatrix.empty(M, C_out, 0, dev), MxMatrix.empty(C_out, inner, 0, dev)
-        self.dX = torch.empty((M, C_in), dtype=dtype, device=dev)
-        self.dW = torch.empty((experts, C_out, C_in) if experts else (C_out, C_in), dtype=torch.float32, device=dev)
-        if experts:
-            need = sq_mx_gemm_experts_wgrad_workspace_size(M, experts, C_out, C_in)
-        else:
-            need = max(sq_mx_gemm_workspace_size(M, C_out, C_in), sq_mx_gemm_workspace_size(M, C_in, C_out),
-                       sq_mx_gemm_workspace_size(C_out, C_in, M))
-        self.ws = _workspace(need, dev)
+        self.dX = torch.empty(self._x_shape, dtype=dtype, device=dev)
+        self.dW = torch.empty(self._w_shape, dtype=torch.float32, device=dev)
+        self.layer = Layer(M, C_in, C_out, experts, _TYPES[dtype], 0)
+        self._held = []     # the layer's pointers stay valid as long as the plan
+        for name in ("w", "w_t", "x", "x_t", "dy", "dy_t"):
+            m = getattr(self, name)
+            self._held += [m.codes, m.scales]
+            setattr(self.layer, name, m.codes.data_ptr())
+            setattr(self.layer, name + "_scales", m.scales.data_ptr())
+        self._layer_ptr, self._dw_ld = ct.addressof(self.layer), max(C_in, 1)
+        self._dx_ptr, self._dw_ptr = self.dX.data_ptr(), self.dW.data_ptr()
+        self._held += [self.Y, self.dX, self.dW]
+        self.ws = _workspace(sq_mx_layer_workspace_size(self.layer), dev)
+        if self.ws is not None:
+            self.layer.workspace, self.layer.workspace_bytes = self.ws.data_ptr(), self.ws.nbytes
 
     def quantize_weight(self, W: torch.Tensor, stream=None) -> None:
         """W [C_out, C_in], or [experts, C_out, C_in]"""
-        _shape(W, (self.experts, self.C_out, self.C_in) if self.experts else (self.C_out, self.C_in), "W")
-        sq_mx_quantize(W, self.w.codes, self.w.scales, self.w_t.codes, self.w_t.scales, stream=stream)
+        if not self.train:
+            raise ValueError("quantize_weight needs a plan with train=True")
+        ld = _checked(W, self._w_shape, self.dtype, "W")
+        _check("sq_mx_layer_weight", self._lib.sq_mx_layer_weight(
+            self._layer_ptr, W.data_ptr(), ld, W.stride(0), _stream(stream)))
 
     def forward(self, x: torch.Tensor, w: Optional[MxMatrix] = None, offsets: Optional[torch.Tensor] = None, stream=None):
-        _shape(x, (self.M, self.C_in), "x")
-        if not self.train:
-            if w is None or (w.rows, w.cols, max(w.stack, 1)) != (self.C_out, self.C_in, max(self.experts, 1)):
-                raise ValueError(f"w: expected codes of {self.experts or 'one'} [{self.C_out}, {self.C_in}]")
-            if w.codes.device != x.device:
-                raise ValueError("w: expected codes on the device of x")
-            sq_mx_linear(x, w.codes, w.scales, self.Y, self.ws, offsets, self.experts, stream)
+        ld = _checked(x, self._x_shape, self.dtype, "x")
+        off = _offsets(offsets, self.experts)
+        if self.train:
+            if w is not None:
+                raise ValueError("w: a training plan has its own codes (quantize_weight)")
+            self.offsets, self._off_ptr = offsets, off
+            _check("sq_mx_layer_forward", self._lib.sq_mx_layer_forward(
+                self._layer_ptr, x.data_ptr(), ld, off, self._y_ptr, self._y_ld, _stream(stream)))
             return self.Y
-        if w is not None:
-            raise ValueError("w: a training plan has its own codes (quantize_weight)")
-        self.offsets = offsets
-        sq_mx_quantize(x, self.x.codes, self.x.scales, self.x_t.codes, self.x_t.scales, offsets, self.experts, stream)
-        self._product(self.x, self.w, self.C_in, self.Y, stream)
+        if w is None or w.rows != self.C_out or w.cols != self.C_in or (w.stack or 1) != (self.experts or 1):
+            raise ValueError(f"w: expected codes of {self.experts or 'one'} [{self.C_out}, {self.C_in}]")
+        codes = w.codes
+        if not codes.is_cuda:
+            raise ValueError("w: expected codes on the GPU")
+        t = self._type
+        _check("sq_mx_linear", self._lib.sq_mx_linear(
+            x.data_ptr(), t, self.M, self.C_in, ld, off, self.experts, codes.data_ptr(), w.scales.data_ptr(), self.C_out,
+            self._y_ptr, t, self._y_ld, *self._ws, _stream(stream)))
         return self.Y
-
-    def _product(self, a: MxMatrix, b: MxMatrix, K: int, C: torch.Tensor, stream) -> None:
-        if self.experts:
-            sq_mx_gemm_experts(a.codes, a.scales, K, self.offsets, self.experts, b.codes, b.scales, C, stream)
-        else:
-            sq_mx_gemm(a.codes, a.scales, b.codes, b.scales, K, C, self.ws, stream)
 
     def backward(self, dy: torch.Tensor, stream=None):
         """(dX, dW) of the last forward"""
         if not self.train:
             raise ValueError("backward needs a plan with train=True")
-        _shape(dy, (self.M, self.C_out), "dy")
-        sq_mx_quantize(dy, self.dy.codes, self.dy.scales, self.dy_t.codes, self.dy_t.scales, self.offsets, self.experts,
-                       stream)
-        self._product(self.dy, self.w_t, self.C_out, self.dX, stream)
-        if self.experts:
-            sq_mx_gemm_experts_wgrad(self.dy_t.codes, self.dy_t.scales, self.x_t.codes, self.x_t.scales, self.M,
-                                     self.offsets, self.experts, self.dW, self.ws, stream)
-        else:
-            sq_mx_gemm(self.dy_t.codes, self.dy_t.scales, self.x_t.codes, self.x_t.scales, self.M, self.dW, self.ws, stream)
+        ld = _checked(dy, self._y_shape, self.dtype, "dy")
+        if self.experts and self.offsets is None:
+            raise ValueError("backward needs a forward before it")
+        _check("sq_mx_layer_backward", self._lib.sq_mx_layer_backward(
+            self._layer_ptr, dy.data_ptr(), ld, self._off_ptr, self._dx_ptr, self._dw_ld, self._dw_ptr, self._dw_ld,
+            _stream(stream)))
         return self.dX, self.dW
 
 
@@ -322,19 +386,25 @@ class ActPlan:
         nc, ns = sq_act_size(M, F, gated)
         self.codes = torch.empty(nc, dtype=torch.int8, device=dev)
         self.scales = torch.empty(ns, dtype=torch.uint8, device=dev)
-        self.H = torch.empty((M, F), dtype=dtype, device=dev)
-        self.dX = torch.empty((M, self.width), dtype=dtype, device=dev)
+        self._h_shape, self._x_shape = torch.Size((M, F)), torch.Size((M, self.width))
+        self.H = torch.empty(self._h_shape, dtype=dtype, device=dev)
+        self.dX = torch.empty(self._x_shape, dtype=dtype, device=dev)
+        self._lib, self._type, self._gated = load(), _TYPES[dtype], int(gated)
+        self._held = (self.codes, self.scales, self.H, self.dX)     # what _ptrs point at
+        self._ptrs = tuple(t.data_ptr() for t in self._held)
+        self._h_ld, self._x_ld = max(F, 1), max(self.width, 1)
 
     def forward(self, x: torch.Tensor, stream=None) -> torch.Tensor:
-        _shape(x, (self.M, self.width), "x")
-        if x.dtype != self.dtype:
-            raise TypeError(f"x: expected {self.dtype}, got {x.dtype}")
-        sq_act_forward(x, self.kind, self.gated, self.H, self.codes, self.scales, stream)
+        ld = _checked(x, self._x_shape, self.dtype, "x")
+        codes, scales, h, _ = self._ptrs
+        _check("sq_act_forward", self._lib.sq_act_forward(
+            x.data_ptr(), self._type, self.kind, self._gated, self.M, self.F, ld, h, self._h_ld, codes, scales, _stream(stream)))
         return self.H
 
     def backward(self, dh: torch.Tensor, stream=None) -> torch.Tensor:
-        _shape(dh, (self.M, self.F), "dh")
-        if dh.dtype != self.dtype:
-            raise TypeError(f"dh: expected {self.dtype}, got {dh.dtype}")
-        sq_act_backward(dh, self.kind, self.gated, self.codes, self.scales, self.dX, stream)
+        ld = _checked(dh, self._h_shape, self.dtype, "dh")
+        codes, scales, _, dx = self._ptrs
+        _check("sq_act_backward", self._lib.sq_act_backward(
+            dh.data_ptr(), self._type, self.kind, self._gated, self.M, self.F, ld, codes, scales, dx, self._x_ld,
+            _stream(stream)))
         return self.dX

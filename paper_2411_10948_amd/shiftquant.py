@@ -50,7 +50,8 @@ EXPORTS = (
     "sq_quantize_grad_noalloc", "sq_conv_dgrad_ranged", "sq_quantize_grad_conv_from_ranges",
     "sq_mx_size", "sq_mx_segment_cols", "sq_mx_quantize", "sq_mx_dequantize", "sq_mx_gemm_workspace_size", "sq_mx_gemm",
     "sq_mx_gemm_experts", "sq_mx_gemm_experts_wgrad_workspace_size", "sq_mx_gemm_experts_wgrad",
-    "sq_mx_linear_workspace_size", "sq_mx_linear", "sq_act_size", "sq_act_forward", "sq_act_backward",
+    "sq_mx_linear_workspace_size", "sq_mx_linear", "sq_mx_layer_workspace_size", "sq_mx_layer_weight",
+    "sq_mx_layer_forward", "sq_mx_layer_backward", "sq_act_size", "sq_act_forward", "sq_act_backward",
     "sq_status_string", "sq_last_error", "sq_last_error_string",
 )
 
@@ -181,6 +182,10 @@ def load() -> ct.CDLL:
         "sq_mx_gemm_experts_wgrad": [_P, _P, _P, _P, _I64, _P, _I64, _I64, _I64, _P, i32, _I64, _P, _SZ, _P],
         "sq_mx_linear_workspace_size": [_I64, _I64, _I64, _I64, ct.POINTER(_SZ)],
         "sq_mx_linear": [_P, i32, _I64, _I64, _I64, _P, _I64, _P, _P, _I64, _P, i32, _I64, _P, _SZ, _P],
+        "sq_mx_layer_workspace_size": [_P, ct.POINTER(_SZ)],
+        "sq_mx_layer_weight": [_P, _P, _I64, _I64, _P],
+        "sq_mx_layer_forward": [_P, _P, _I64, _P, _P, _I64, _P],
+        "sq_mx_layer_backward": [_P, _P, _I64, _P, _P, _I64, _P, _I64, _P],
         "sq_act_size": [_I64, _I64, i32, ct.POINTER(_SZ), ct.POINTER(_SZ)],
         "sq_act_forward": [_P, i32, i32, i32, _I64, _I64, _I64, _P, _I64, _P, _P, _P],
         "sq_act_backward": [_P, i32, i32, i32, _I64, _I64, _I64, _P, _P, _P, _I64, _P],

@@ -359,14 +359,14 @@ def test_offsets_out_of_order_stay_in_the_buffers(mx, off):
     for key in ("Y", "dX", "dW"):
         t = getattr(plan, key)
         big = torch.full((t.numel() + 2048,), 5.0, device="cuda")
-        setattr(plan, key, big[1024:1024 + t.numel()].view(t.shape))
+        setattr(plan, f"_{key.lower()}_ptr", big[1024:].data_ptr())
         guard[key] = big
-    for m in (plan.x, plan.x_t, plan.dy, plan.dy_t):
+    for name in ("x", "x_t", "dy", "dy_t"):
         for f in ("codes", "scales"):
-            t = getattr(m, f)
+            t = getattr(getattr(plan, name), f)
             big = torch.full((t.numel() + 8192,), 5, dtype=torch.uint8, device="cuda")
-            setattr(m, f, big[4096:4096 + t.numel()].view(t.shape))
-            guard[id(m), f] = big
+            setattr(plan.layer, name + ("_scales" if f == "scales" else ""), big[4096:].data_ptr())
+            guard[name, f] = big
     plan.quantize_weight(w)
     plan.forward(x, offsets=o)
     plan.backward(dy)

@@ -133,11 +133,33 @@ def test_refusals(mx):
     assert gw(rows=1 << 23) == UNSUPPORTED and gw(off=None) == INVALID and gw(ldc=63) == INVALID and gw(e=0) == INVALID
     assert gw(M=0) == 0
 
-    def lin(X=p, M=100, K=64, ld=64, off=None, e=0, N=64, Y=p, ldy=64, ws=p, nws=1 << 40):
+    def lin(X=p, M=4096, K=512, ld=512, off=None, e=0, N=512, Y=p, ldy=512, ws=p, nws=1 << 40):
         return L.sq_mx_linear(X, 1, M, K, ld, off, e, p, p, N, Y, 1, ldy, ws, nws, None)
 
-    assert lin(X=None) == INVALID and lin(ld=63) == INVALID and lin(ldy=63) == INVALID and lin(ws=None) == INVALID
+    assert lin(X=None) == INVALID and lin(ld=511) == INVALID and lin(ldy=511) == INVALID and lin(ws=None) == INVALID
     assert lin(nws=16) == SMALL and lin(off=p) == INVALID and lin(M=0) == 0
+
+    from paper_2411_10948_amd.mx import Layer
+    def layer(**kw):
+        names = [f[0] for f in Layer._fields_]
+        v = dict(rows=65536, c_in=64, c_out=64, experts=0, type=0, reserved=0, workspace_bytes=1 << 40)
+        return Layer(*({**{n: 0x100000 for n in names}, **v, **kw}[n] for n in names))
+    ref_ = lambda **kw: ct.byref(layer(**kw))
+    assert L.sq_mx_layer_workspace_size(None, ct.byref(n)) == INVALID
+    assert L.sq_mx_layer_workspace_size(ref_(type=7), ct.byref(n)) == INVALID
+    assert L.sq_mx_layer_workspace_size(ref_(rows=1 << 23), ct.byref(n)) == UNSUPPORTED
+    assert L.sq_mx_layer_workspace_size(ref_(), ct.byref(n)) == 0 and n.value > 0      # dW of one tile, 512 steps
+    assert L.sq_mx_layer_weight(ref_(), None, 64, 0, None) == INVALID
+    assert L.sq_mx_layer_weight(ref_(), p, 63, 0, None) == INVALID
+    assert L.sq_mx_layer_forward(ref_(), None, 64, None, p, 64, None) == INVALID
+    assert L.sq_mx_layer_forward(ref_(), p, 64, p, p, 64, None) == INVALID             # offsets without experts
+    assert L.sq_mx_layer_forward(ref_(experts=2), p, 64, None, p, 64, None) == INVALID
+    assert L.sq_mx_layer_forward(ref_(), p, 64, None, p, 63, None) == INVALID
+    assert L.sq_mx_layer_forward(ref_(x_t=0x100008), p, 64, None, p, 64, None) == INVALID
+    assert L.sq_mx_layer_forward(ref_(workspace_bytes=16), p, 64, None, p, 64, None) == SMALL
+    back = lambda l, dY=p, dX=p, dW=p, ldw=64: L.sq_mx_layer_backward(l, dY, 64, None, dX, 64, dW, ldw, None)
+    assert back(ref_(), dY=None) == INVALID and back(ref_(), dX=None) == INVALID and back(ref_(), dW=None) == INVALID
+    assert back(ref_(), ldw=63) == INVALID and back(ref_(w_t=None)) == INVALID and back(ref_(workspace=None)) == INVALID
 
     def af(X=p, kind=0, gated=1, M=4, F=64, ldx=128, H=p, ldh=64, c=p, s=p):
         return L.sq_act_forward(X, 0, kind, gated, M, F, ldx, H, ldh, c, s, None)
