@@ -68,7 +68,6 @@ struct MxGemmArgs {
     int type;
     int64_t ldc;                           // kExpertInner: matrix e at e * M * ldc
     float* part;                           // split-K partials [splits, M, N] (kDense)
-    bool stream_out;                       // fp32 C past the caches: a weight gradient, which the optimizer reads later
 };
 int64_t mx_gemm_splits(const MxGemmArgs& a);      // K splits of the product (1 unless kDense)
 hipError_t launch_mx_gemm(const MxGemmArgs& a, hipStream_t s);

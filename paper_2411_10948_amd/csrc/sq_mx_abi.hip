@@ -314,7 +314,6 @@ sq_status sq_mx_gemm_experts_wgrad(const uint8_t* A, const uint8_t* A_scales, co
         a.C = C;
         a.type = type;
         a.ldc = ldc;
-        a.stream_out = true;
         return hip_status(launch_mx_gemm(a, static_cast<hipStream_t>(stream)), "mx weight gradient by expert");
     });
 }
@@ -400,7 +399,6 @@ static void backward_args(const sq_mx_layer* l, MxGemmArgs& x, MxGemmArgs& w) {
     w.mode = l->experts ? kExpertInner : kDense;
     w.experts = (int)l->experts;
     w.rows = l->rows;
-    w.stream_out = true;
 }
 
 static size_t layer_workspace(const sq_mx_layer* l) {

@@ -40,24 +40,28 @@ __device__ __forceinline__ void wait_loads() {
 }
 
 // Block tile BM x BN of WM x WN waves, a ring of STAGES stages of 128 inner
-// elements in LDS.
-template <int BM_, int BN_, int WM_, int WN_, int STAGES_>
+// elements in LDS.  AHEAD: a stage's operands are read into registers while
+// the one before is multiplied, which a wave of 64 x 128 outputs needs (two
+// waves a SIMD); the smaller ones read and multiply in turn, with the registers
+// for more blocks a CU instead.
+template <int BM_, int BN_, int STAGES_, bool AHEAD_, int BLOCKS>
 struct MxCfg {
-    static constexpr int BM = BM_, BN = BN_, WM = WM_, WN = WN_, STAGES = STAGES_;
-    static constexpr int kWaves = WM * WN, kThreads = 64 * kWaves;
+    static constexpr int BM = BM_, BN = BN_, WM = 2, WN = 2, STAGES = STAGES_;
+    static constexpr bool AHEAD = AHEAD_;
+    static constexpr int kWaves = WM * WN, kThreads = 64 * kWaves, kOccupancy = BLOCKS * kWaves / 4;
     static constexpr int TM = BM / WM, TN = BN / WN, FM = TM / 16, FN = TN / 16;
     static constexpr int kGroups = (BM + BN) / 16;            // 16-row operand groups of a stage
     static constexpr int LPW = kGroups / kWaves;              // 1 KB loads per wave per stage
     static constexpr int kStage = kGroups * kMxTileBytes;
     static constexpr int kSmem = STAGES * kStage;
     static constexpr int kCycle = STAGES == 3 ? 24 : 8;       // steps after which stage, buffer and scale byte recur
-    static_assert(LPW * kWaves == kGroups && TM % 16 == 0 && TN % 16 == 0, "even split");
     static_assert(BM / 16 % kWaves == 0 && BN / 16 % kWaves == 0, "a wave's i-th loads are all of A or all of B");
-    static_assert(STAGES == 3 || STAGES == 4, "ring");
+    static_assert(STAGES >= 2 && STAGES <= 4 && BLOCKS * kSmem <= 160 * 1024, "ring");
 };
-using MxLarge = MxCfg<256, 256, 4, 2, 3>;   // 8 waves of 64 x 128, 96 KB: one block per CU
-using MxMid = MxCfg<128, 128, 2, 2, 3>;     // 4 waves of 64 x 64, 48 KB: three
-using MxSmall = MxCfg<64, 64, 2, 2, 4>;     // 4 waves of 32 x 32, 32 KB: five
+using MxWide = MxCfg<128, 256, 3, true, 2>;    // waves of 64 x 128
+using MxMid = MxCfg<128, 128, 3, false, 3>;    // waves of 64 x 64
+using MxShort = MxCfg<128, 128, 2, false, 4>;  // the same, a block more a CU for a step less in flight
+using MxSmall = MxCfg<64, 64, 4, true, 5>;     // waves of 32 x 32
 
 __device__ __forceinline__ void store_out(void* C, int type, int64_t at, float v) {
     if (type == SQ_TYPE_F32) static_cast<float*>(C)[at] = v;
@@ -176,10 +180,10 @@ __device__ __forceinline__ void product(const MxProduct& d, uint32_t block, uint
     for (int i = 0; i < T::FM; ++i)
 #pragma unroll
         for (int j = 0; j < T::FN; ++j) acc[i][j] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
-    // Operands of a stage in registers, two buffers: stage t + 1 is read while
-    // stage t is multiplied.  The scales of four tiles, one word a fragment,
+    // Operands of a stage in registers (AHEAD: two buffers).  The scales of four tiles, one word a fragment,
     // come straight from memory, two buffers too.
-    v4i fa[2][T::FM], fb[2][T::FN];
+    constexpr int kBufs = T::AHEAD ? 2 : 1;
+    v4i fa[kBufs][T::FM], fb[kBufs][T::FN];
     int sa[2][T::FM], sb[2][T::FN];
     auto load_scales = [&](int unit, auto BUF) {
         constexpr int buf = decltype(BUF)::value;
@@ -206,35 +210,49 @@ __device__ __forceinline__ void product(const MxProduct& d, uint32_t block, uint
         for (int j = 0; j < T::FN; ++j)
             fb[buf][j] = *reinterpret_cast<const v4i*>(st + (T::BM / 16 + wn * T::FN + j) * kMxTileBytes);
     };
-    // Step t, of index S in the cycle: publish stage t + 1, refill stage t's
-    // place (its operands were read in the step before), read stage t + 1's
-    // operands, multiply stage t's.
-    auto step = [&](int t, auto S) {
-        constexpr int s = decltype(S)::value, nxt = (s + 1) % T::STAGES, buf = s & 1, grp = (s >> 2) & 1;
-        wait_loads<(T::STAGES - 2) * T::LPW>();
-        __builtin_amdgcn_s_barrier();
-        if constexpr ((s & 3) == 0) load_scales((t >> 2) + 1, std::integral_constant<int, grp ^ 1>());
-        issue(t + T::STAGES, s % T::STAGES);
-        read_frags(std::integral_constant<int, nxt>(), std::integral_constant<int, buf ^ 1>());
+    auto multiply = [&](auto S, auto BUF) {
+        constexpr int s = decltype(S)::value, buf = decltype(BUF)::value, grp = (s >> 2) & 1;
 #pragma unroll
         for (int j = 0; j < T::FN; ++j)
 #pragma unroll
             for (int i = 0; i < T::FM; ++i)
                 acc[i][j] = mfma4<(s & 3)>(fb[buf][j], fa[buf][i], acc[i][j], sb[grp][j], sa[grp][i]);
-        constexpr int kReads = T::FM + T::FN, kMfma = T::FM * T::FN, kPer = kMfma / kReads > 0 ? kMfma / kReads : 1;
+    };
+    // Step t, of index S in the cycle.
+    auto step = [&](int t, auto S) {
+        constexpr int s = decltype(S)::value, grp = (s >> 2) & 1, buf = s & 1;
+        wait_loads<(T::STAGES - 2) * T::LPW>();
+        __builtin_amdgcn_s_barrier();
+        if constexpr ((s & 3) == 0) load_scales((t >> 2) + 1, std::integral_constant<int, grp ^ 1>());
+        if constexpr (T::AHEAD) {
+            // stage t + 1 is there; refill stage t's place (its operands were
+            // read in the step before), read stage t + 1's operands, multiply stage t's
+            issue(t + T::STAGES, s % T::STAGES);
+            read_frags(std::integral_constant<int, (s + 1) % T::STAGES>(), std::integral_constant<int, buf ^ 1>());
+            multiply(S, std::integral_constant<int, buf>());
+            constexpr int kReads = T::FM + T::FN, kMfma = T::FM * T::FN, kPer = kMfma / kReads > 0 ? kMfma / kReads : 1;
 #pragma unroll
-        for (int g = 0; g < kReads; ++g) {
-            __builtin_amdgcn_sched_group_barrier(0x008, kPer, 0);   // MFMAs
-            __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);      // one LDS read
+            for (int g = 0; g < kReads; ++g) {
+                __builtin_amdgcn_sched_group_barrier(0x008, kPer, 0);   // MFMAs
+                __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);      // one LDS read
+            }
+        } else {
+            // stage t is there; read its operands, refill the place of stage t - 1, multiply
+            read_frags(std::integral_constant<int, s % T::STAGES>(), std::integral_constant<int, 0>());
+            issue(t + T::STAGES - 1, (s + T::STAGES - 1) % T::STAGES);
+            multiply(S, std::integral_constant<int, 0>());
         }
     };
     if (n > 0) {
         load_scales(0, std::integral_constant<int, 0>());
+        constexpr int kFirst = T::AHEAD ? T::STAGES : T::STAGES - 1;
 #pragma unroll
-        for (int i = 0; i < T::STAGES; ++i) issue(i, i);
-        wait_loads<(T::STAGES - 1) * T::LPW>();
-        __builtin_amdgcn_s_barrier();
-        read_frags(std::integral_constant<int, 0>(), std::integral_constant<int, 0>());
+        for (int i = 0; i < kFirst; ++i) issue(i, i);
+        if constexpr (T::AHEAD) {
+            wait_loads<(T::STAGES - 1) * T::LPW>();
+            __builtin_amdgcn_s_barrier();
+            read_frags(std::integral_constant<int, 0>(), std::integral_constant<int, 0>());
+        }
         for (int t = 0; t < n; t += T::kCycle)
             unrolled_steps<T::kCycle>([&](auto S) {
                 constexpr int s = decltype(S)::value;
@@ -245,6 +263,10 @@ __device__ __forceinline__ void product(const MxProduct& d, uint32_t block, uint
     }
 
     // ---- epilogue: 16 rows of a wave at a time through LDS, out in whole lines ----
+    // Nontemporal: the lines of C that ordinary stores leave in the last-level
+    // cache evict dirty ones.  Weight gradients of 16 experts, 32768 rows, 4096 x
+    // 2048: 258 -> 188 us; 32768 x 4096 outputs in bf16 and the quantizer that
+    // reads them next, together 268 -> 254 us; 3152 x 768 in fp32, 17.1 -> 15.8.
     __builtin_amdgcn_s_waitcnt(0);
     __builtin_amdgcn_s_barrier();
     constexpr int kLd = T::TN + 4;
@@ -284,12 +306,11 @@ __device__ __forceinline__ void product(const MxProduct& d, uint32_t block, uint
                 if (row >= row_end || col >= p.N) continue;
                 if (vec && col + kCols <= p.N) {
                     if constexpr (f32) {
-                        v4f* to = reinterpret_cast<v4f*>(static_cast<float*>(C) + at);
-                        if (p.stream_out) __builtin_nontemporal_store(a, to);
-                        else *to = a;
+                        __builtin_nontemporal_store(a, reinterpret_cast<v4f*>(static_cast<float*>(C) + at));
                     } else {
-                        *reinterpret_cast<uint4*>(static_cast<uint16_t*>(C) + at) =
-                            make_uint4(bf16_pair(a.x, a.y), bf16_pair(a.z, a.w), bf16_pair(b.x, b.y), bf16_pair(b.z, b.w));
+                        const v4i w = {(int)bf16_pair(a.x, a.y), (int)bf16_pair(a.z, a.w), (int)bf16_pair(b.x, b.y),
+                                       (int)bf16_pair(b.z, b.w)};
+                        __builtin_nontemporal_store(w, reinterpret_cast<v4i*>(static_cast<uint16_t*>(C) + at));
                     }
                 } else {
 #pragma unroll
@@ -305,7 +326,7 @@ __device__ __forceinline__ void product(const MxProduct& d, uint32_t block, uint
 #endif
 
 template <class T, int MODE>
-__global__ __launch_bounds__(T::kThreads, 2) void k_mx_gemm(MxProduct d) {
+__global__ __launch_bounds__(T::kThreads, T::kOccupancy) void k_mx_gemm(MxProduct d) {
 #if defined(__HIP_DEVICE_COMPILE__)
     __shared__ __attribute__((aligned(1024))) uint8_t smem[T::kSmem];
     product<T, MODE>(d, blockIdx.x, smem);
@@ -316,7 +337,7 @@ __global__ __launch_bounds__(T::kThreads, 2) void k_mx_gemm(MxProduct d) {
 // input and weight gradients.  The second's blocks fill the CUs that the
 // first one's last tiles leave idle.
 template <class T, int MODE_A, int MODE_B>
-__global__ __launch_bounds__(T::kThreads, 2) void k_mx_gemm_pair(MxProduct a, MxProduct b) {
+__global__ __launch_bounds__(T::kThreads, T::kOccupancy) void k_mx_gemm_pair(MxProduct a, MxProduct b) {
 #if defined(__HIP_DEVICE_COMPILE__)
     __shared__ __attribute__((aligned(1024))) uint8_t smem[T::kSmem];
     if (blockIdx.x < a.blocks) product<T, MODE_A>(a, blockIdx.x, smem);
@@ -485,26 +506,26 @@ __global__ __launch_bounds__(64 * kRowsWaves, 4) void k_mx_rows(MxRowsArgs p, ui
 #endif
 }
 
-enum MxTileKind { kLarge, kMid, kSmall };
+enum MxTileKind { kWide, kMid, kShort, kSmall };
 
-// Time of a dense product in us: rounds of one 256 x 256 tile a CU, or of three
-// 128 x 128 tiles a CU, which go on as each ends; a step of 128 inner elements
-// and what a tile costs besides (fitted to 4 to 1376 tiles of 4 to 86 steps).
-// 8192 x 4096 x 11008: 157 us in large tiles, 178 in mid ones;
-// 4096 x 2048 x 4096: 29 and 22.
-bool large_tiles(const MxGemmArgs& a) {
-    const double k = (double)((a.K + kMxTile - 1) / kMxTile);
-    const int64_t large = ((a.M + 255) / 256) * ((a.N + 255) / 256), mid = ((a.M + 127) / 128) * ((a.N + 127) / 128);
-    return mid >= 768 && 1.1 * (double)((large + 255) / 256) * (0.84 * k + 4.5) < (double)mid / 768.0 * (0.74 * k + 4.0);
-}
-
-// 128 x 128 tiles where they give nearly every CU one, else 64 x 64
-// (2048 x 2048 x 512, 256 tiles: 6.4 us and 6.8; 768 x 768 x 3152, 36: 10.0
-// and 6.1; by expert 2048 rows, 64 experts, 2048 x 1024: 20.5 and 21.6).
+// Tiles by the size of the product, each rule with the times in us of the
+// kinds on either side of it.
+//   Small below 240 tiles of 128 x 128: 768 x 768 x 3152 (36 tiles) small 6.1,
+//     mid 10.0; 2048 x 2048 x 512 (256) small 6.8, mid 6.4.
+//   Wide from 12 steps of 128 inner elements on, where its tiles waste little of
+//     the columns and of the last round over the CUs: 8192 x 11008 x 4096 wide
+//     186, mid 198; 4096 x 2048 x 4096 22.4 and 22.7; 3000 x 3000 x 3000 (288
+//     tiles) 28.6 and 24.8; 16384 x 1536 x 768 (6 steps) 20.7 and 19.9.
+//   Short up to 8 steps: 8192 x 8192 x 512 short 35.4, mid 37.1;
+//     1024 x 8192 x 2048 (16 steps) 16.2 and 15.5.
 MxTileKind tile_kind(const MxGemmArgs& a) {
-    if (a.mode == kDense && large_tiles(a)) return kLarge;
+    const int64_t times = a.mode == kExpertInner ? a.experts : 1;
     const int64_t tm = a.mode == kExpertRows ? a.M / 128 + std::min<int64_t>(a.experts, a.M) : (a.M + 127) / 128;
-    return tm * ((a.N + 127) / 128) * (a.mode == kExpertInner ? a.experts : 1) >= 240 ? kMid : kSmall;
+    if (tm * ((a.N + 127) / 128) * times < 240) return kSmall;
+    const int64_t k = a.mode == kExpertInner ? a.rows / a.experts : a.K, steps = (k + kMxTile - 1) / kMxTile;
+    const int64_t tn = (a.N + 255) / 256, wide = tm * tn * times, rounds = (wide + 255) / 256;
+    if (steps >= 12 && 20 * 256 * tn <= 21 * a.N && 100 * 256 * rounds <= 135 * wide) return kWide;
+    return steps <= 8 ? kShort : kMid;
 }
 
 template <class T, int MODE>
@@ -536,9 +557,9 @@ hipError_t gemm(const MxGemmArgs& a, hipStream_t s) {
 template <int MODE>
 hipError_t gemm_mode(const MxGemmArgs& a, hipStream_t s) {
     switch (tile_kind(a)) {
-        case kLarge:
-            if constexpr (MODE == kDense) return gemm<MxLarge, MODE>(a, s);
+        case kWide: return gemm<MxWide, MODE>(a, s);
         case kMid: return gemm<MxMid, MODE>(a, s);
+        case kShort: return gemm<MxShort, MODE>(a, s);
         default: return gemm<MxSmall, MODE>(a, s);
     }
 }
@@ -597,12 +618,23 @@ hipError_t launch_mx_gemm(const MxGemmArgs& a, hipStream_t s) {
 }
 
 hipError_t launch_mx_gemm_pair(const MxGemmArgs& a, const MxGemmArgs& b, hipStream_t s) {
-    const MxTileKind k = tile_kind(a);
-    if (k == tile_kind(b) && a.M > 0 && a.N > 0 && b.M > 0 && b.N > 0) {
-        if (a.mode == kDense)
-            return k == kLarge ? pair<MxLarge, kDense, kDense>(a, b, s)
-                   : k == kMid ? pair<MxMid, kDense, kDense>(a, b, s) : pair<MxSmall, kDense, kDense>(a, b, s);
-        return k == kMid ? pair<MxMid, kExpertRows, kExpertInner>(a, b, s) : pair<MxSmall, kExpertRows, kExpertInner>(a, b, s);
+    const MxTileKind ka = tile_kind(a), kb = tile_kind(b);
+    const bool both = a.M > 0 && a.N > 0 && b.M > 0 && b.N > 0;
+    if (both && ka == kb && a.mode == kDense) {
+        switch (ka) {
+            case kWide: return pair<MxWide, kDense, kDense>(a, b, s);
+            case kMid: return pair<MxMid, kDense, kDense>(a, b, s);
+            case kShort: return pair<MxShort, kDense, kDense>(a, b, s);
+            default: return pair<MxSmall, kDense, kDense>(a, b, s);
+        }
+    }
+    if (both && ka == kb) {
+        switch (ka) {
+            case kWide: return pair<MxWide, kExpertRows, kExpertInner>(a, b, s);
+            case kMid: return pair<MxMid, kExpertRows, kExpertInner>(a, b, s);
+            case kShort: return pair<MxShort, kExpertRows, kExpertInner>(a, b, s);
+            default: return pair<MxSmall, kExpertRows, kExpertInner>(a, b, s);
+        }
     }
     const hipError_t e = launch_mx_gemm(a, s);
     return e == hipSuccess ? launch_mx_gemm(b, s) : e;
