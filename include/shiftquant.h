@@ -723,8 +723,8 @@ sq_status sq_mx_segment_cols(int64_t rows, int64_t experts, int64_t* cols);
  * Either pair may be NULL, not both.  With offsets (batch == 1): codes_t is
  * [cols, sq_mx_segment_cols(rows, experts)], its blocks start anew at each
  * expert's first row.
- * Errors: SQ_ERR_INVALID_ARGUMENT, SQ_ERR_UNSUPPORTED (rows >= 2^23 with
- * codes_t), SQ_ERR_HIP.
+ * Errors: SQ_ERR_INVALID_ARGUMENT, SQ_ERR_UNSUPPORTED (with codes_t: rows >=
+ * 2^23, or sq_mx_segment_cols >= 2^24), SQ_ERR_HIP.
  * ------------------------------------------------------------------------- */
 sq_status sq_mx_quantize(const void* X, int32_t type, int64_t batch, int64_t rows, int64_t cols, int64_t ld, int64_t stride,
                          const int32_t* offsets, int64_t experts,

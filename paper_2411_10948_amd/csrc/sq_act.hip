@@ -17,11 +17,11 @@ namespace {
 // 8 consecutive elements as they came, 4 words of bf16 pairs or 8 of fp32;
 // columns at and past `cols` read as zero.
 template <typename T>
-__device__ __forceinline__ void load8(const T* row, int64_t c, int64_t cols, bool vec, uint32_t* w) {
-    if (vec && c + 8 <= cols) {
+__device__ __forceinline__ void load8(const T* row, int64_t c, int64_t cols, uint32_t* w) {
+    if (c + 8 <= cols) {
 #pragma unroll
         for (int i = 0; i < (int)(8 * sizeof(T) / 4); i += 4) {
-            const uint4 v = *reinterpret_cast<const uint4*>(row + c + i * 4 / sizeof(T));
+            const u32x4_any v = *reinterpret_cast<const u32x4_any*>(row + c + i * 4 / sizeof(T));
             w[i] = v.x;
             w[i + 1] = v.y;
             w[i + 2] = v.z;
@@ -44,14 +44,14 @@ __device__ __forceinline__ void values8(const uint32_t* w, float* f) {
 }
 
 template <typename T>
-__device__ __forceinline__ void store8(T* row, int64_t c, int64_t cols, bool vec, const float* f) {
-    if (vec && c + 8 <= cols) {
+__device__ __forceinline__ void store8(T* row, int64_t c, int64_t cols, const float* f) {
+    if (c + 8 <= cols) {
+        u32x4_any* to = reinterpret_cast<u32x4_any*>(row + c);
         if constexpr (sizeof(T) == 4) {
-            reinterpret_cast<float4*>(row + c)[0] = make_float4(f[0], f[1], f[2], f[3]);
-            reinterpret_cast<float4*>(row + c)[1] = make_float4(f[4], f[5], f[6], f[7]);
+            __builtin_nontemporal_store(u32x4_any{__float_as_uint(f[0]), __float_as_uint(f[1]), __float_as_uint(f[2]), __float_as_uint(f[3])}, to);
+            __builtin_nontemporal_store(u32x4_any{__float_as_uint(f[4]), __float_as_uint(f[5]), __float_as_uint(f[6]), __float_as_uint(f[7])}, to + 1);
         } else {
-            *reinterpret_cast<uint4*>(row + c) =
-                make_uint4(bf16_pair(f[0], f[1]), bf16_pair(f[2], f[3]), bf16_pair(f[4], f[5]), bf16_pair(f[6], f[7]));
+            __builtin_nontemporal_store(u32x4_any{bf16_pair(f[0], f[1]), bf16_pair(f[2], f[3]), bf16_pair(f[4], f[5]), bf16_pair(f[6], f[7])}, to);
         }
     } else {
 #pragma unroll
@@ -124,7 +124,6 @@ __device__ __forceinline__ void from_copy8(const int8_t* codes, const uint8_t* s
 struct ActGrid {
     uint32_t items, chunks, mul;
     int shift;
-    bool vec;
 };
 __device__ __forceinline__ uint32_t row_of(const ActGrid& g, uint32_t i) {
     return (uint32_t)(((uint64_t)i * g.mul) >> (31 + g.shift));
@@ -144,8 +143,8 @@ __global__ __launch_bounds__(256) void k_act_forward(ActArgs p, ActGrid q) {
     constexpr int kWords = 8 * sizeof(T) / 4;
     uint32_t gw[kWords], uw[kWords];
     float g[8], u[8], h[8];
-    load8<T>(x, c, p.F, q.vec, gw);
-    if constexpr (GATED) load8<T>(x + p.F, c, p.F, q.vec, uw);
+    load8<T>(x, c, p.F, gw);
+    if constexpr (GATED) load8<T>(x + p.F, c, p.F, uw);
     const bool first = (threadIdx.x & 3) == 0;
     values8<T>(gw, g);
     copy8<T>(gw, g, codes + c, scales + (c >> 5), first);
@@ -159,7 +158,7 @@ __global__ __launch_bounds__(256) void k_act_forward(ActArgs p, ActGrid q) {
         h[e] = g[e] * gate<KIND>(g[e], slope);
         if constexpr (GATED) h[e] *= u[e];
     }
-    store8<T>(static_cast<T*>(p.h) + r * p.ld_h, c, p.F, q.vec, h);
+    store8<T>(static_cast<T*>(p.h) + r * p.ld_h, c, p.F, h);
 }
 
 template <typename T, int KIND, bool GATED>
@@ -173,7 +172,7 @@ __global__ __launch_bounds__(256) void k_act_backward(ActArgs p, ActGrid q) {
     const uint8_t* scales = p.scales + r * (ldc / 32);
     uint32_t dw[8 * sizeof(T) / 4];
     float g[8], u[8], d[8];
-    load8<T>(static_cast<const T*>(p.h) + r * p.ld_h, c, p.F, q.vec, dw);
+    load8<T>(static_cast<const T*>(p.h) + r * p.ld_h, c, p.F, dw);
     from_copy8(codes + c, scales + (c >> 5), g);
     if constexpr (GATED) from_copy8(codes + fp + c, scales + ((fp + c) >> 5), u);
     values8<T>(dw, d);
@@ -190,17 +189,15 @@ __global__ __launch_bounds__(256) void k_act_backward(ActArgs p, ActGrid q) {
         }
     }
     T* dx = static_cast<T*>(p.dx) + r * p.ld_x;
-    store8<T>(dx, c, p.F, q.vec, g);
-    if constexpr (GATED) store8<T>(dx + p.F, c, p.F, q.vec, u);
+    store8<T>(dx, c, p.F, g);
+    if constexpr (GATED) store8<T>(dx + p.F, c, p.F, u);
 }
 
 template <typename T, int KIND, bool GATED>
 hipError_t act(const ActArgs& args, bool forward, hipStream_t s) {
     ActArgs a = args;
     const int64_t chunks = round_up(a.F, 32) / 8, fp = chunks * 8, codes_ld = GATED ? 2 * fp : fp;
-    auto ok = [](const void* p, int64_t ld) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0 && (ld * sizeof(T)) % 16 == 0; };
     ActGrid q{};
-    q.vec = ok(forward ? a.x : a.dx, a.ld_x) && ok(a.h, a.ld_h) && (!GATED || (a.F * sizeof(T)) % 16 == 0);
     q.chunks = (uint32_t)chunks;
     while (((int64_t)1 << q.shift) < chunks) ++q.shift;
     q.mul = (uint32_t)((((uint64_t)1 << (31 + q.shift)) + (uint64_t)chunks - 1) / (uint64_t)chunks);

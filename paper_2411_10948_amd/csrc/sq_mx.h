@@ -197,6 +197,11 @@ __device__ __forceinline__ void segment_inner(const int32_t* offsets, int expert
     }
 }
 
+// 16 bytes at any element's address: gfx950 loads and stores them unaligned, so
+// odd row strides and views need no path of their own.
+typedef uint32_t u32x4_any __attribute__((ext_vector_type(4), aligned(2)));
+typedef float f32x4_any __attribute__((ext_vector_type(4), aligned(4)));
+
 __device__ __forceinline__ float bf16_value(uint32_t b) { return __uint_as_float(b << 16); }
 // round to nearest even; NaN stays NaN
 __device__ __forceinline__ uint32_t bf16_pair(float a, float b) {

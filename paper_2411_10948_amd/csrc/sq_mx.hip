@@ -93,7 +93,7 @@ struct QuantTile<uint16_t> {   // bf16 bits
 // vector instructions bound the kernel, not HBM, when each element was
 // unpacked and multiplied by the scale's inverse (8192 x 11008 both ways 84 us).
 template <typename T>
-__global__ __launch_bounds__(256) void k_mx_quantize(MxQuantArgs p, uint32_t tiles_c, bool vec) {
+__global__ __launch_bounds__(256) void k_mx_quantize(MxQuantArgs p, uint32_t tiles_c) {
     constexpr int TC = QuantTile<T>::TC, kLanes = TC / 8, kPass = 64 / kLanes, kPasses = 32 / kPass;
     constexpr int kWords = 8 * sizeof(T) / 4;            // words a lane loads of a row
     constexpr int kCols = 4 / sizeof(T);                 // columns a lane takes of the transpose
@@ -120,10 +120,15 @@ __global__ __launch_bounds__(256) void k_mx_quantize(MxQuantArgs p, uint32_t til
     for (int i = 0; i < kPasses; ++i) {
         const int64_t r = row0 + r0 + i * kPass;
         const T* src = x + r * p.ld + c;
-        if (r < row_end && vec && c + 8 <= p.cols) {
+        if (r < row_end && c + 8 <= p.cols) {
 #pragma unroll
-            for (int w = 0; w < kWords; w += 4)
-                *reinterpret_cast<uint4*>(&v[i][w]) = *reinterpret_cast<const uint4*>(src + w * 4 / sizeof(T));
+            for (int w = 0; w < kWords; w += 4) {
+                const u32x4_any l = *reinterpret_cast<const u32x4_any*>(src + w * 4 / sizeof(T));
+                v[i][w] = l.x;
+                v[i][w + 1] = l.y;
+                v[i][w + 2] = l.z;
+                v[i][w + 3] = l.w;
+            }
         } else {
             T t[8];
 #pragma unroll
@@ -256,9 +261,7 @@ hipError_t quantize(const MxQuantArgs& a, hipStream_t s) {
     // whole 128-element tiles of the columns, so that the row codes' padding is written too
     const int64_t tiles_c = round_up(a.cols, kMxTile) / TC;
     const int64_t tiles_r = a.offsets ? a.rows / 128 + std::min<int64_t>(a.experts, a.rows) : (a.rows + 127) / 128;
-    const bool vec = (reinterpret_cast<uintptr_t>(a.x) & 15) == 0 && (a.ld * sizeof(T)) % 16 == 0 &&
-                     (a.batch == 1 || (a.stride * sizeof(T)) % 16 == 0);
-    k_mx_quantize<T><<<dim3((uint32_t)(tiles_r * tiles_c), (uint32_t)a.batch), 256, 0, s>>>(a, (uint32_t)tiles_c, vec);
+    k_mx_quantize<T><<<dim3((uint32_t)(tiles_r * tiles_c), (uint32_t)a.batch), 256, 0, s>>>(a, (uint32_t)tiles_c);
     return hipGetLastError();
 }
 

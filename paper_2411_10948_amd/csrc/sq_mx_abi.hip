@@ -19,7 +19,7 @@ using namespace sq;
 
 constexpr int64_t kMaxRows = (int64_t)1 << 31;
 constexpr int64_t kMaxCols = (int64_t)1 << 20;
-constexpr int64_t kMaxInner = (int64_t)1 << 23;     // a product's inner axis: 16-row group offsets of a tile in 31 bits
+constexpr int64_t kMaxInner = (int64_t)1 << 23;     // a product's inner axis: a tile's 16 groups, 8 bytes an element, in 31 bits
 constexpr int64_t kMaxExperts = (int64_t)1 << 16;
 constexpr double kMaxBlocks = 2147483647.0;         // of one launch
 
@@ -70,6 +70,14 @@ sq_status check_experts(const int32_t* offsets, int64_t experts) {
 
 sq_status check_inner(int64_t k) {
     if (k >= kMaxInner) return fail(SQ_ERR_UNSUPPORTED, "the inner axis has 2^23 elements or more");
+    return SQ_OK;
+}
+
+// the inner axis of a transpose by expert: whole units for each, twice as long at most
+sq_status check_segments(int64_t rows, int64_t experts) {
+    SQ_TRY(check_inner(rows));
+    if (mx_segment_cols(rows, experts) >= 2 * kMaxInner)
+        return fail(SQ_ERR_UNSUPPORTED, "the experts' rows, each rounded up to 512, are 2^24 or more");
     return SQ_OK;
 }
 
@@ -171,7 +179,7 @@ sq_status sq_mx_quantize(const void* X, int32_t type, int64_t batch, int64_t row
         if (codes || scales) SQ_TRY(check_mx(codes, scales, "codes"));
         if (codes_t || scales_t) {
             SQ_TRY(check_mx(codes_t, scales_t, "codes_t"));
-            SQ_TRY(check_inner(rows));
+            SQ_TRY(experts ? check_segments(rows, experts) : check_inner(rows));
         }
         SQ_TRY(check_values(X, type, ld, cols, "X"));
         if (batch > 1 && (stride < 0 || stride < (rows - 1) * ld + cols)) return invalid("stride is smaller than a matrix");
@@ -276,8 +284,8 @@ sq_status sq_mx_gemm_experts(const uint8_t* A, const uint8_t* A_scales, int64_t 
 sq_status sq_mx_gemm_experts_wgrad_workspace_size(int64_t rows, int64_t experts, int64_t M, int64_t N, size_t* bytes) {
     return guarded([&]() -> sq_status {
         SQ_TRY(check_dim(rows, kMaxRows, "rows"));
-        SQ_TRY(check_inner(rows));
         if (experts < 1 || experts >= kMaxExperts) return invalid("experts is out of range");
+        SQ_TRY(check_segments(rows, experts));
         SQ_TRY(check_dim(M, kMaxCols, "M"));
         SQ_TRY(check_dim(N, kMaxCols, "N"));
         if (!bytes) return invalid("bytes is NULL");
@@ -381,7 +389,7 @@ static sq_status check_layer(const sq_mx_layer* l) {
     SQ_TRY(check_dim(l->rows, kMaxRows, "rows"));
     SQ_TRY(check_dim(l->c_in, kMaxCols, "c_in"));
     SQ_TRY(check_dim(l->c_out, kMaxCols, "c_out"));
-    return check_inner(l->rows);
+    return l->experts ? check_segments(l->rows, l->experts) : check_inner(l->rows);
 }
 
 static sq_status check_layer_offsets(const sq_mx_layer* l, const int32_t* offsets) {
@@ -502,7 +510,7 @@ static sq_status check_act(int32_t type, int32_t kind, int32_t gated, int64_t M,
     if (M == 0 || F == 0) return SQ_OK;
     if (ld_x < F * (gated ? 2 : 1)) return invalid("the row stride of X or dX is smaller than its row");
     if (ld_h < F) return invalid("the row stride of H or dH is smaller than its row");
-    return check_blocks(M, 1, F, 2048, 0, 1);
+    return SQ_OK;
 }
 
 static sq_status check_copy(const int8_t* codes, const uint8_t* scales) {

@@ -282,8 +282,6 @@ __device__ __forceinline__ void product(const MxProduct& d, uint32_t block, uint
         ldc = p.N;
         base = split * p.M * p.N;
     }
-    const int esz = type == SQ_TYPE_F32 ? 4 : 2;
-    const bool vec = (ldc * esz) % 16 == 0 && (reinterpret_cast<uintptr_t>(C) & 15) == 0 && (base * esz) % 16 == 0;
     const int64_t n_w = n0 + wn * T::TN;
 #pragma unroll
     for (int i = 0; i < T::FM; ++i) {
@@ -304,13 +302,12 @@ __device__ __forceinline__ void product(const MxProduct& d, uint32_t block, uint
                 if constexpr (!f32) b = *reinterpret_cast<const v4f*>(src + 4);
                 const int64_t row = m + r, col = n_w + kCols * q, at = base + row * ldc + col;
                 if (row >= row_end || col >= p.N) continue;
-                if (vec && col + kCols <= p.N) {
+                if (col + kCols <= p.N) {
                     if constexpr (f32) {
-                        __builtin_nontemporal_store(a, reinterpret_cast<v4f*>(static_cast<float*>(C) + at));
+                        __builtin_nontemporal_store((f32x4_any)a, reinterpret_cast<f32x4_any*>(static_cast<float*>(C) + at));
                     } else {
-                        const v4i w = {(int)bf16_pair(a.x, a.y), (int)bf16_pair(a.z, a.w), (int)bf16_pair(b.x, b.y),
-                                       (int)bf16_pair(b.z, b.w)};
-                        __builtin_nontemporal_store(w, reinterpret_cast<v4i*>(static_cast<uint16_t*>(C) + at));
+                        const u32x4_any w = {bf16_pair(a.x, a.y), bf16_pair(a.z, a.w), bf16_pair(b.x, b.y), bf16_pair(b.z, b.w)};
+                        __builtin_nontemporal_store(w, reinterpret_cast<u32x4_any*>(static_cast<uint16_t*>(C) + at));
                     }
                 } else {
 #pragma unroll
@@ -408,8 +405,7 @@ __device__ __forceinline__ v4i quantize_lane(const uint32_t* w, int& scale_byte)
     return a;
 }
 
-// VEC: X's rows are whole aligned 16-byte pieces.
-template <typename T, bool VEC, int FN, int U>
+template <typename T, int FN, int U>
 __global__ __launch_bounds__(64 * kRowsWaves, 4) void k_mx_rows(MxRowsArgs p, uint32_t tiles_n) {
 #if defined(__HIP_DEVICE_COMPILE__)
     constexpr int kLd = 16 * FN + 4, kWords = 32 * sizeof(T) / 4, kV = 16 / sizeof(T);
@@ -437,55 +433,62 @@ __global__ __launch_bounds__(64 * kRowsWaves, 4) void k_mx_rows(MxRowsArgs p, ui
     v4f acc[FN];
 #pragma unroll
     for (int j = 0; j < FN; ++j) acc[j] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
-    for (int t = beg; t < end; t += U) {
+    auto load_w = [&](int at, int j, v4i& w, int& ws) {
+        const uint32_t grp = (uint32_t)min(j, last);
+        w = __builtin_bit_cast(v4i, __builtin_amdgcn_raw_buffer_load_b128(rW, 16u * (uint32_t)lane,
+                                                                          (int)(grp * gb) + at * kMxTileBytes, 0));
+        ws = (int)__builtin_amdgcn_raw_buffer_load_b32(rWs, 4u * (uint32_t)lane, (int)(grp * gs) + (at >> 2) * kMxUnitScales, 0);
+    };
+    const int full = K / kMxTile, stop = min(end, full);    // whole tiles
+    for (int t = beg; t < stop; t += U) {
         v4i w[U][FN];
         int ws[U][FN];
 #pragma unroll
-        for (int u = 0; u < U; ++u) {
-            const int at = min(t + u, end - 1);
+        for (int u = 0; u < U; ++u)
 #pragma unroll
-            for (int j = 0; j < FN; ++j) {
-                const uint32_t grp = (uint32_t)min(j, last);
-                w[u][j] = __builtin_bit_cast(v4i, __builtin_amdgcn_raw_buffer_load_b128(
-                                                      rW, 16u * (uint32_t)lane, (int)(grp * gb) + at * kMxTileBytes, 0));
-                ws[u][j] = (int)__builtin_amdgcn_raw_buffer_load_b32(rWs, 4u * (uint32_t)lane,
-                                                                     (int)(grp * gs) + (at >> 2) * kMxUnitScales, 0);
-            }
-        }
+            for (int j = 0; j < FN; ++j) load_w(min(t + u, stop - 1), j, w[u][j], ws[u][j]);
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            const int at = min(t + u, end - 1), c = at * kMxTile + (lane >> 4) * 32;
-            const bool tail = (at + 1) * kMxTile > K;
+            const int at = min(t + u, stop - 1);
             uint32_t v[kWords];
-            if constexpr (VEC) {
 #pragma unroll
-                for (int q = 0; q < 32 / kV; ++q) {
-                    const uint4 l = *reinterpret_cast<const uint4*>(x + min(c + q * kV, K - kV));
-                    v[4 * q] = l.x;
-                    v[4 * q + 1] = l.y;
-                    v[4 * q + 2] = l.z;
-                    v[4 * q + 3] = l.w;
-                }
-            } else {
-#pragma unroll
-                for (int q = 0; q < kWords; ++q) {
-                    if constexpr (sizeof(T) == 4) v[q] = __float_as_uint(x[min(c + q, K - 1)]);
-                    else v[q] = (uint32_t)x[min(c + 2 * q, K - 1)] | (uint32_t)x[min(c + 2 * q + 1, K - 1)] << 16;
-                }
-            }
-            if (tail) {     // columns past the end count as zeros
-#pragma unroll
-                for (int q = 0; q < kWords; ++q) {
-                    const int k = c + q * (4 / (int)sizeof(T));
-                    v[q] &= k >= K ? 0u : (sizeof(T) == 2 && k + 1 == K) ? 0xFFFFu : 0xFFFFFFFFu;
-                }
+            for (int q = 0; q < 32 / kV; ++q) {
+                const u32x4_any l = *reinterpret_cast<const u32x4_any*>(x + at * kMxTile + (lane >> 4) * 32 + q * kV);
+                v[4 * q] = l.x;
+                v[4 * q + 1] = l.y;
+                v[4 * q + 2] = l.z;
+                v[4 * q + 3] = l.w;
             }
             int sa;
             v4i a = quantize_lane<sizeof(T) == 2>(v, sa);
-            if (t + u >= end) a = v4i{0, 0, 0, 0}, sa = 0;     // this part's tiles are done
+            if (t + u >= stop) a = v4i{0, 0, 0, 0}, sa = 0;     // read again to keep the loads free of branches
             const int byte = 8 * (at & 3);
 #pragma unroll
             for (int j = 0; j < FN; ++j) acc[j] = mfma4<0>(w[u][j], a, acc[j], ws[u][j] >> byte, sa);
+        }
+    }
+    if (end > stop && end == n && beg < end) {      // the tile that K ends in, element by element
+        const int c = full * kMxTile + (lane >> 4) * 32;
+        uint32_t v[kWords];
+#pragma unroll
+        for (int q = 0; q < kWords; ++q) {
+            if constexpr (sizeof(T) == 4) {
+                const uint32_t e = __float_as_uint(x[min(c + q, K - 1)]);
+                v[q] = c + q < K ? e : 0u;
+            } else {
+                const uint32_t lo = x[min(c + 2 * q, K - 1)], hi = x[min(c + 2 * q + 1, K - 1)];
+                v[q] = (c + 2 * q < K ? lo : 0u) | (c + 2 * q + 1 < K ? hi << 16 : 0u);
+            }
+        }
+        int sa;
+        const v4i a = quantize_lane<sizeof(T) == 2>(v, sa);
+        const int byte = 8 * (full & 3);
+#pragma unroll
+        for (int j = 0; j < FN; ++j) {
+            v4i w;
+            int ws;
+            load_w(full, j, w, ws);
+            acc[j] = mfma4<0>(w, a, acc[j], ws >> byte, sa);
         }
     }
     // a lane holds columns 4 (lane / 16).. of row lane % 16
@@ -587,23 +590,22 @@ int64_t mx_gemm_splits(const MxGemmArgs& a) {
 
 namespace {
 
-template <typename T, bool VEC, int FN, int U>
-hipError_t rows(const MxRowsArgs& a, hipStream_t s) {
+template <typename T, int FN, int U>
+hipError_t rows(const MxRowsArgs& a, int64_t tiles_m, hipStream_t s) {
     const int64_t tiles_n = (a.N + 16 * FN - 1) / (16 * FN);
-    const int64_t tiles_m = a.offsets ? a.M / 16 + std::min<int64_t>(a.experts, a.M) : (a.M + 15) / 16;
-    k_mx_rows<T, VEC, FN, U><<<(uint32_t)(tiles_m * tiles_n), 64 * kRowsWaves, 0, s>>>(a, (uint32_t)tiles_n);
+    k_mx_rows<T, FN, U><<<(uint32_t)(tiles_m * tiles_n), 64 * kRowsWaves, 0, s>>>(a, (uint32_t)tiles_n);
     return hipGetLastError();
 }
 
+// 64 columns a block where blocks of 16 would be more than two a CU (one row,
+// 4096 -> 11008, 688 of them: 7.5 us against 8.3; 64 experts, 64 rows, 2048 ->
+// 1024: 12.4 against 16.3; one row, 4096 -> 4096, 256: 5.6 against 4.7).  fp32
+// values fill the registers with one tile in flight.
 template <typename T>
 hipError_t rows_of(const MxRowsArgs& a, hipStream_t s) {
-    const int64_t sz = sizeof(T);
-    const bool vec = (reinterpret_cast<uintptr_t>(a.x) & 15) == 0 && (a.ld * sz) % 16 == 0 && (a.K * sz) % 16 == 0 && a.K > 0;
     const int64_t tiles_m = a.offsets ? a.M / 16 + std::min<int64_t>(a.experts, a.M) : (a.M + 15) / 16;
-    const bool wide = tiles_m * ((a.N + 15) / 16) >= 512;
     constexpr int U = sizeof(T) == 4 ? 1 : 2;
-    if (!vec) return rows<T, false, 1, 1>(a, s);
-    return wide ? rows<T, true, 4, U>(a, s) : rows<T, true, 1, U>(a, s);
+    return tiles_m * ((a.N + 15) / 16) >= 512 ? rows<T, 4, U>(a, tiles_m, s) : rows<T, 1, U>(a, tiles_m, s);
 }
 
 }  // namespace
