@@ -28,9 +28,11 @@ __device__ __forceinline__ void load8(const T* row, int64_t c, int64_t cols, uin
             w[i + 3] = v.w;
         }
     } else {
-        T v[8];
+        T v[8];     // loads without branches, those past the end cleared
 #pragma unroll
-        for (int e = 0; e < 8; ++e) v[e] = c + e < cols ? row[c + e] : (T)0;
+        for (int e = 0; e < 8; ++e) v[e] = row[min(c + e, cols - 1)];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] = c + e < cols ? v[e] : (T)0;
         __builtin_memcpy(w, v, sizeof(v));
     }
 }

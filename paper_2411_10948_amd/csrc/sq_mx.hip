@@ -115,12 +115,16 @@ __global__ __launch_bounds__(256) void k_mx_quantize(MxQuantArgs p, uint32_t til
 
     const int q = lane % kLanes, r0 = wave * 32 + lane / kLanes;
     const int64_t c = col0 + 8 * q;
+    const int left = (int)(p.cols - c);
     uint32_t v[kPasses][kWords];
 #pragma unroll
     for (int i = 0; i < kPasses; ++i) {
         const int64_t r = row0 + r0 + i * kPass;
         const T* src = x + r * p.ld + c;
-        if (r < row_end && c + 8 <= p.cols) {
+#pragma unroll
+        for (int w = 0; w < kWords; ++w) v[i][w] = 0;
+        if (r >= row_end || left <= 0) continue;
+        if (left >= 8) {
 #pragma unroll
             for (int w = 0; w < kWords; w += 4) {
                 const u32x4_any l = *reinterpret_cast<const u32x4_any*>(src + w * 4 / sizeof(T));
@@ -129,10 +133,12 @@ __global__ __launch_bounds__(256) void k_mx_quantize(MxQuantArgs p, uint32_t til
                 v[i][w + 2] = l.z;
                 v[i][w + 3] = l.w;
             }
-        } else {
+        } else {    // the last columns: loads without branches, those past the end cleared
             T t[8];
 #pragma unroll
-            for (int e = 0; e < 8; ++e) t[e] = r < row_end && c + e < p.cols ? src[e] : (T)0;
+            for (int e = 0; e < 8; ++e) t[e] = src[min(e, left - 1)];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) t[e] = e < left ? t[e] : (T)0;
             __builtin_memcpy(v[i], t, sizeof(t));
         }
     }
