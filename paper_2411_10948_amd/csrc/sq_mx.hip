@@ -92,7 +92,7 @@ struct QuantTile<uint16_t> {   // bf16 bits
 // from load to code (maximum, conversion), which halves the instructions;
 // vector instructions bound the kernel, not HBM, when each element was
 // unpacked and multiplied by the scale's inverse (8192 x 11008 both ways 84 us).
-template <typename T>
+template <typename T, bool NT>
 __global__ __launch_bounds__(256) void k_mx_quantize(MxQuantArgs p, uint32_t tiles_c) {
     constexpr int TC = QuantTile<T>::TC, kLanes = TC / 8, kPass = 64 / kLanes, kPasses = 32 / kPass;
     constexpr int kWords = 8 * sizeof(T) / 4;            // words a lane loads of a row
@@ -127,7 +127,10 @@ __global__ __launch_bounds__(256) void k_mx_quantize(MxQuantArgs p, uint32_t til
         if (left >= 8) {
 #pragma unroll
             for (int w = 0; w < kWords; w += 4) {
-                const u32x4_any l = *reinterpret_cast<const u32x4_any*>(src + w * 4 / sizeof(T));
+                const u32x4_any* at = reinterpret_cast<const u32x4_any*>(src + w * 4 / sizeof(T));
+                u32x4_any l;
+                if constexpr (NT) l = __builtin_nontemporal_load(at);
+                else l = *at;
                 v[i][w] = l.x;
                 v[i][w + 1] = l.y;
                 v[i][w + 2] = l.z;
@@ -267,7 +270,15 @@ hipError_t quantize(const MxQuantArgs& a, hipStream_t s) {
     // whole 128-element tiles of the columns, so that the row codes' padding is written too
     const int64_t tiles_c = round_up(a.cols, kMxTile) / TC;
     const int64_t tiles_r = a.offsets ? a.rows / 128 + std::min<int64_t>(a.experts, a.rows) : (a.rows + 127) / 128;
-    k_mx_quantize<T><<<dim3((uint32_t)(tiles_r * tiles_c), (uint32_t)a.batch), 256, 0, s>>>(a, (uint32_t)tiles_c);
+    // Inputs that the last-level cache would not keep anyway are read past it, so
+    // that the codes stay there for the product: 8192 x 4096 in bf16 and its product
+    // with 11008 columns 208 -> 195 us; a step of 3152 x 768 x 768 in fp32 29.0 ->
+    // 31.9 with such loads.
+    const dim3 grid((uint32_t)(tiles_r * tiles_c), (uint32_t)a.batch);
+    if ((double)a.batch * (double)a.rows * (double)a.cols * sizeof(T) >= 32e6)
+        k_mx_quantize<T, true><<<grid, 256, 0, s>>>(a, (uint32_t)tiles_c);
+    else
+        k_mx_quantize<T, false><<<grid, 256, 0, s>>>(a, (uint32_t)tiles_c);
     return hipGetLastError();
 }
 

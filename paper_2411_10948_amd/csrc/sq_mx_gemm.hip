@@ -620,26 +620,30 @@ hipError_t launch_mx_gemm(const MxGemmArgs& a, hipStream_t s) {
 }
 
 hipError_t launch_mx_gemm_pair(const MxGemmArgs& a, const MxGemmArgs& b, hipStream_t s) {
-    const MxTileKind ka = tile_kind(a), kb = tile_kind(b);
-    const bool both = a.M > 0 && a.N > 0 && b.M > 0 && b.N > 0;
-    if (both && ka == kb && a.mode == kDense) {
+    MxTileKind ka = tile_kind(a), kb = tile_kind(b);
+    // A product of few tiles goes along in the other one's: 1187 rows on 12
+    // experts, 520 x 1000, dX in 64 x 64 tiles 5.9 us and dW in 128 x 128 9.9.
+    if (ka == kSmall) ka = kb;
+    if (kb == kSmall) kb = ka;
+    if (ka != kb || a.M == 0 || a.N == 0 || b.M == 0 || b.N == 0) {
+        const hipError_t e = launch_mx_gemm(a, s);
+        return e == hipSuccess ? launch_mx_gemm(b, s) : e;
+    }
+    if (a.mode == kDense) {     // the longer tiles first
+        const MxGemmArgs &x = a.K >= b.K ? a : b, &y = a.K >= b.K ? b : a;
         switch (ka) {
-            case kWide: return pair<MxWide, kDense, kDense>(a, b, s);
-            case kMid: return pair<MxMid, kDense, kDense>(a, b, s);
-            case kShort: return pair<MxShort, kDense, kDense>(a, b, s);
-            default: return pair<MxSmall, kDense, kDense>(a, b, s);
+            case kWide: return pair<MxWide, kDense, kDense>(x, y, s);
+            case kMid: return pair<MxMid, kDense, kDense>(x, y, s);
+            case kShort: return pair<MxShort, kDense, kDense>(x, y, s);
+            default: return pair<MxSmall, kDense, kDense>(x, y, s);
         }
     }
-    if (both && ka == kb) {
-        switch (ka) {
-            case kWide: return pair<MxWide, kExpertRows, kExpertInner>(a, b, s);
-            case kMid: return pair<MxMid, kExpertRows, kExpertInner>(a, b, s);
-            case kShort: return pair<MxShort, kExpertRows, kExpertInner>(a, b, s);
-            default: return pair<MxSmall, kExpertRows, kExpertInner>(a, b, s);
-        }
+    switch (ka) {
+        case kWide: return pair<MxWide, kExpertRows, kExpertInner>(a, b, s);
+        case kMid: return pair<MxMid, kExpertRows, kExpertInner>(a, b, s);
+        case kShort: return pair<MxShort, kExpertRows, kExpertInner>(a, b, s);
+        default: return pair<MxSmall, kExpertRows, kExpertInner>(a, b, s);
     }
-    const hipError_t e = launch_mx_gemm(a, s);
-    return e == hipSuccess ? launch_mx_gemm(b, s) : e;
 }
 
 // Few rows: at most 16 (an expert, on average), or so few blocks of 16 rows and

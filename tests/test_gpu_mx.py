@@ -192,6 +192,62 @@ def test_gemm_of_many_tiles(mx, M, N, K):
     _close(C.double().cpu().numpy(), want, mag, K, "f32")
 
 
+@pytest.mark.parametrize("M,K,N,E", [
+    (4096, 2048, 4096, 0),      # 128 x 256 tiles, both gradients in one launch
+    (2000, 1300, 2100, 0),      # 128 x 128, 11 steps
+    (2300, 700, 2050, 0),       # 128 x 128, 6 steps; ragged in every direction
+    (4500, 65, 70, 0),          # few tiles of a long inner axis: split
+    (6400, 2048, 2048, 3), (9000, 1300, 1300, 6), (6000, 1000, 1000, 8), (3000, 1700, 2048, 3), (700, 200, 150, 3)])
+def test_training_step_of_every_tile_shape(mx, M, K, N, E):
+    # against fp64 products of the values that the step's own codes stand for (the quantizer's tests check those)
+    import torch
+    g = torch.Generator(device="cuda").manual_seed(M)
+    r = lambda *s: torch.randn(*s, generator=g, device="cuda").bfloat16()
+    x, dy, w = r(M, K), r(M, N), r(*((E, N, K) if E else (N, K)))
+    off, o = [0, M], None
+    if E:
+        cut = torch.randint(0, M + 1, (E - 1,), generator=g, device="cuda").sort().values.tolist()
+        off = [0, *cut, M]
+        o = torch.tensor(off, dtype=torch.int32, device="cuda")
+    plan = mx.LinearPlan(M, K, N, experts=E, train=True)
+    for t in (plan.Y, plan.dX, plan.dW):
+        t.fill_(float("nan"))
+    plan.quantize_weight(w)
+    y = plan.forward(x, offsets=o)
+    dx, dw = plan.backward(dy)
+
+    def close(got, a, b, terms):
+        want, mag = a @ b.T, a.abs() @ b.abs().T
+        tol = mag * (terms + 2) * 2.0 ** -23
+        if got.dtype == torch.bfloat16:
+            tol = tol + (want.abs() + tol) * 2.0 ** -8
+        assert ((got.double() - want).abs() <= tol).all()
+    xv, dv = plan.x.values().double(), plan.dy.values().double()
+    wv, tv = plan.w.values().double(), plan.w_t.values().double()
+    for e, (lo, hi) in enumerate(ref.segments(off)):
+        s = slice(lo, hi)
+        if hi == lo:
+            assert not dw[e].any()
+            continue
+        close(y[s], xv[s], wv[e] if E else wv, K)
+        close(dx[s], dv[s], tv[e] if E else tv, N)
+        a, b = (mx.quantize(t[s], False, True)[1].values().double() for t in (dy, x))
+        close(dw[e] if E else dw, a, b, hi - lo)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_quantize_large_inputs(mx, dtype):
+    # inputs of 32 MB and more are read past the last-level cache; compared with the same rows in smaller pieces
+    import torch
+    M, C = 4224, 4097 if dtype == "bf16" else 2049
+    x = torch.randn(M, C, generator=torch.Generator(device="cuda").manual_seed(1), device="cuda").to(_dtype(dtype))
+    a, t = mx.quantize(x, True, True)
+    a, t = a.values(), t.values()
+    for r in range(0, M, 1056):
+        pa, pt = mx.quantize(x[r:r + 1056], True, True)
+        assert torch.equal(a[r:r + 1056], pa.values()) and torch.equal(t[:, r:r + 1056], pt.values())
+
+
 def test_gemm_scales_of_every_size(mx):
     # scales from 2^-127 up: products underflow to zero or overflow as fp32 does
     import torch
@@ -439,6 +495,17 @@ def test_graph_replay(mx, M, K, N, E, train):
         for a, b in zip(out, want):
             assert torch.equal(a, b)
     assert x2 is not None
+
+
+@pytest.mark.parametrize("M", [1, 16, 5000])
+@pytest.mark.parametrize("K,N", [(0, 70), (1, 1), (70, 0)])
+def test_no_columns(mx, M, K, N):
+    import torch
+    plan = mx.LinearPlan(M, K, N, dtype=torch.float32)
+    plan.Y.fill_(3.0)
+    w = torch.ones(N, K, device="cuda")
+    y = plan.forward(torch.ones(M, K, device="cuda"), mx.quantize(w)[0])
+    assert y.shape == (M, N) and (y == K).all()         # a sum over no columns is 0
 
 
 def test_empty(mx):
