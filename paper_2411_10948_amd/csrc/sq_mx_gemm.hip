@@ -44,16 +44,17 @@ __device__ __forceinline__ void wait_loads() {
 // the one before is multiplied, which a wave of 64 x 128 outputs needs (two
 // waves a SIMD); the smaller ones read and multiply in turn, with the registers
 // for more blocks a CU instead.
-template <int BM_, int BN_, int STAGES_, bool AHEAD_, int BLOCKS>
+template <int BM_, int BN_, int STAGES_, bool AHEAD_, int BLOCKS, int WM_ = 2>
 struct MxCfg {
-    static constexpr int BM = BM_, BN = BN_, WM = 2, WN = 2, STAGES = STAGES_;
-    static constexpr bool AHEAD = AHEAD_;
+    static constexpr int BM = BM_, BN = BN_, WM = WM_, WN = 2, STAGES = STAGES_;
+    static constexpr bool AHEAD = AHEAD_, kScalesInLds = BN >= 128;
     static constexpr int kWaves = WM * WN, kThreads = 64 * kWaves, kOccupancy = BLOCKS * kWaves / 4;
     static constexpr int TM = BM / WM, TN = BN / WN, FM = TM / 16, FN = TN / 16;
     static constexpr int kGroups = (BM + BN) / 16;            // 16-row operand groups of a stage
     static constexpr int LPW = kGroups / kWaves;              // 1 KB loads per wave per stage
     static constexpr int kStage = kGroups * kMxTileBytes;
-    static constexpr int kSmem = STAGES * kStage;
+    static constexpr int kScales = kScalesInLds ? BN / 16 * kMxUnitScales : 0;   // of B, four tiles
+    static constexpr int kSmem = STAGES * kStage + 2 * kScales;
     static constexpr int kCycle = STAGES == 3 ? 24 : 8;       // steps after which stage, buffer and scale byte recur
     static_assert(BM / 16 % kWaves == 0 && BN / 16 % kWaves == 0, "a wave's i-th loads are all of A or all of B");
     static_assert(STAGES >= 2 && STAGES <= 4 && BLOCKS * kSmem <= 160 * 1024, "ring");
@@ -184,7 +185,7 @@ __device__ __forceinline__ void product(const MxProduct& d, uint32_t block, uint
     // come straight from memory, two buffers too.
     constexpr int kBufs = T::AHEAD ? 2 : 1;
     v4i fa[kBufs][T::FM], fb[kBufs][T::FN];
-    int sa[2][T::FM], sb[2][T::FN];
+    int sa[2][T::FM], sb[T::kScalesInLds ? 1 : 2][T::FN];
     auto load_scales = [&](int unit, auto BUF) {
         constexpr int buf = decltype(BUF)::value;
         const int k = ((int)(t0 >> 2) + min(unit, (n - 1) >> 2)) * kMxUnitScales;
@@ -198,8 +199,27 @@ __device__ __forceinline__ void product(const MxProduct& d, uint32_t block, uint
         }
 #pragma unroll
         for (int j = 0; j < T::FN; ++j)
-            sb[buf][j] = (int)__builtin_amdgcn_raw_buffer_load_b32(rBs, 4u * (uint32_t)lane,
-                                                                   (int)((uint32_t)min(wn * T::FN + j, last_b) * gs) + k, 0);
+            if constexpr (!T::kScalesInLds)
+                sb[buf][j] = (int)__builtin_amdgcn_raw_buffer_load_b32(rBs, 4u * (uint32_t)lane,
+                                                                       (int)((uint32_t)min(wn * T::FN + j, last_b) * gs) + k, 0);
+        // B's, 1 KB of four groups at a time, to LDS
+        if constexpr (T::kScalesInLds) {
+            constexpr int kLoads = T::BN / 64;
+#pragma unroll
+            for (int q = 0; q < (kLoads + T::kWaves - 1) / T::kWaves; ++q) {
+                const int at = q * T::kWaves + wave;
+                if (kLoads % T::kWaves == 0 || at < kLoads)
+                    __builtin_amdgcn_raw_ptr_buffer_load_lds(
+                        rBs, (lds_void_t*)(smem + T::STAGES * T::kStage + (unit & 1) * T::kScales + at * 1024), 16,
+                        (uint32_t)min(4 * at + (lane >> 4), last_b) * gs + 16u * ((uint32_t)lane & 15u), k, 0, 0);
+            }
+        }
+    };
+    auto read_scales = [&](int unit) {
+        const uint8_t* ss = smem + T::STAGES * T::kStage + (unit & 1) * T::kScales + wn * T::FN * kMxUnitScales + 4 * lane;
+#pragma unroll
+        for (int j = 0; j < T::FN; ++j)
+            if constexpr (T::kScalesInLds) sb[0][j] = *reinterpret_cast<const int*>(ss + j * kMxUnitScales);
     };
     auto read_frags = [&](auto STG, auto BUF) {
         constexpr int stg = decltype(STG)::value, buf = decltype(BUF)::value;
@@ -216,14 +236,17 @@ __device__ __forceinline__ void product(const MxProduct& d, uint32_t block, uint
         for (int j = 0; j < T::FN; ++j)
 #pragma unroll
             for (int i = 0; i < T::FM; ++i)
-                acc[i][j] = mfma4<(s & 3)>(fb[buf][j], fa[buf][i], acc[i][j], sb[grp][j], sa[grp][i]);
+                acc[i][j] = mfma4<(s & 3)>(fb[buf][j], fa[buf][i], acc[i][j], sb[T::kScalesInLds ? 0 : grp][j], sa[grp][i]);
     };
     // Step t, of index S in the cycle.
     auto step = [&](int t, auto S) {
         constexpr int s = decltype(S)::value, grp = (s >> 2) & 1, buf = s & 1;
         wait_loads<(T::STAGES - 2) * T::LPW>();
         __builtin_amdgcn_s_barrier();
-        if constexpr ((s & 3) == 0) load_scales((t >> 2) + 1, std::integral_constant<int, grp ^ 1>());
+        if constexpr ((s & 3) == 0) {
+            read_scales(t >> 2);
+            load_scales((t >> 2) + 1, std::integral_constant<int, grp ^ 1>());
+        }
         if constexpr (T::AHEAD) {
             // stage t + 1 is there; refill stage t's place (its operands were
             // read in the step before), read stage t + 1's operands, multiply stage t's
