@@ -354,14 +354,29 @@ __global__ __launch_bounds__(T::kThreads, T::kOccupancy) void k_mx_gemm(MxProduc
 }
 
 // Two products that do not depend on each other, in one launch: a layer's
-// input and weight gradients.  The second's blocks fill the CUs that the
-// first one's last tiles leave idle.
+// input and weight gradients.  Dense, one after the other (alternating blocks
+// share less of the L2: the step of 8192 x 4096 x 11008 622 -> 680 us).  By
+// expert their blocks alternate, eight of one at a time (one for each XCD), in
+// proportion: a weight gradient over few rows is bound by its stores, which go
+// along with the products of the other (32768 rows, 16 experts, 785 -> 756).
 template <class T, int MODE_A, int MODE_B>
 __global__ __launch_bounds__(T::kThreads, T::kOccupancy) void k_mx_gemm_pair(MxProduct a, MxProduct b) {
 #if defined(__HIP_DEVICE_COMPILE__)
     __shared__ __attribute__((aligned(1024))) uint8_t smem[T::kSmem];
-    if (blockIdx.x < a.blocks) product<T, MODE_A>(a, blockIdx.x, smem);
-    else product<T, MODE_B>(b, blockIdx.x - a.blocks, smem);
+    const uint32_t na = (a.blocks + kXcds - 1) / kXcds, nb = (b.blocks + kXcds - 1) / kXcds;
+    const uint32_t c = blockIdx.x / kXcds, lane = blockIdx.x % kXcds;
+    uint32_t of_a = min(c, na);                 // eights of a before this one
+    bool is_a = c < na;
+    if constexpr (MODE_B == kExpertInner) {
+        of_a = (uint32_t)((uint64_t)c * na / (na + nb));
+        is_a = (uint32_t)((uint64_t)(c + 1) * na / (na + nb)) > of_a;
+    }
+    const uint32_t i = (is_a ? of_a : c - of_a) * kXcds + lane;
+    if (is_a) {
+        if (i < a.blocks) product<T, MODE_A>(a, i, smem);
+    } else {
+        if (i < b.blocks) product<T, MODE_B>(b, i, smem);
+    }
 #endif
 }
 
@@ -594,7 +609,7 @@ template <class T, int MODE_A, int MODE_B>
 hipError_t pair(const MxGemmArgs& a, const MxGemmArgs& b, hipStream_t s) {
     const int splits_a = (int)mx_gemm_splits(a), splits_b = (int)mx_gemm_splits(b);
     const MxProduct da = product_of<T, MODE_A>(a, splits_a), db = product_of<T, MODE_B>(b, splits_b);
-    k_mx_gemm_pair<T, MODE_A, MODE_B><<<da.blocks + db.blocks, T::kThreads, 0, s>>>(da, db);
+    k_mx_gemm_pair<T, MODE_A, MODE_B><<<(uint32_t)(round_up(da.blocks, 8) + round_up(db.blocks, 8)), T::kThreads, 0, s>>>(da, db);
     hipError_t e = hipGetLastError();
     if (e == hipSuccess && splits_a > 1) e = reduce(a, splits_a, s);
     return e == hipSuccess && splits_b > 1 ? reduce(b, splits_b, s) : e;
