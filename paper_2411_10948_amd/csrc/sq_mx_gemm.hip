@@ -8,6 +8,14 @@
 // in fp32.  The operand layout (sq_mx.h) is the instruction's, so a tile goes
 // from memory to LDS and from LDS to registers in lane order: contiguous
 // 1 KB loads and conflict-free reads, no swizzle.
+//
+// What bounds the large products is power: the register-only loop of the
+// instruction runs at 8.9 PFLOP/s on constant operands and at 5.8 to 6.1 on
+// random ones, as the shader clock falls to about 1.45 GHz.  The whole kernel
+// reaches 4.8 at 8192 x 4096 x 44032 (5.8 on zeros), 4.1 to 4.5 at 8192 x 4096 x
+// 11008 (164 to 180 us) and 3.7 at 8192 x 11008 x 4096 (197 us, a bf16 library
+// product of the same size 3.2 times as long); without the loop's loads from
+// the L2 it would be at the power limit, without their waits no faster.
 #include <algorithm>
 #include <type_traits>
 
@@ -44,9 +52,9 @@ __device__ __forceinline__ void wait_loads() {
 // the one before is multiplied, which a wave of 64 x 128 outputs needs (two
 // waves a SIMD); the smaller ones read and multiply in turn, with the registers
 // for more blocks a CU instead.
-template <int BM_, int BN_, int STAGES_, bool AHEAD_, int BLOCKS, int WM_ = 2>
+template <int BM_, int BN_, int STAGES_, bool AHEAD_, int BLOCKS>
 struct MxCfg {
-    static constexpr int BM = BM_, BN = BN_, WM = WM_, WN = 2, STAGES = STAGES_;
+    static constexpr int BM = BM_, BN = BN_, WM = 2, WN = 2, STAGES = STAGES_;
     static constexpr bool AHEAD = AHEAD_, kScalesInLds = BN >= 128;
     static constexpr int kWaves = WM * WN, kThreads = 64 * kWaves, kOccupancy = BLOCKS * kWaves / 4;
     static constexpr int TM = BM / WM, TN = BN / WN, FM = TM / 16, FN = TN / 16;
@@ -181,8 +189,10 @@ __device__ __forceinline__ void product(const MxProduct& d, uint32_t block, uint
     for (int i = 0; i < T::FM; ++i)
 #pragma unroll
         for (int j = 0; j < T::FN; ++j) acc[i][j] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
-    // Operands of a stage in registers (AHEAD: two buffers).  The scales of four tiles, one word a fragment,
-    // come straight from memory, two buffers too.
+    // Operands of a stage in registers (AHEAD: two buffers).  The scales of
+    // four tiles, one word a fragment: A's straight from memory, two buffers; B's
+    // through LDS where the tile is wide, 1 KB a load (with a load a fragment the
+    // 32768-row product by expert of 4096 -> 2048 took 156 us, now 147).
     constexpr int kBufs = T::AHEAD ? 2 : 1;
     v4i fa[kBufs][T::FM], fb[kBufs][T::FN];
     int sa[2][T::FM], sb[T::kScalesInLds ? 1 : 2][T::FN];
@@ -397,9 +407,10 @@ __global__ __launch_bounds__(256) void k_mx_reduce(const float* part, int splits
 // layout is the matrix instruction's, so a wave loads 16 x 128 tiles of W
 // straight into registers, 1 KB at a time.  A block owns 16 rows (of one
 // expert) and 16 FN columns; its eight waves share the inner axis in contiguous
-// parts, four tiles of W in flight each.  A lane reads the 32 elements of X of
-// its row and block and quantizes them in registers.  The waves' sums meet in
-// LDS in a fixed order.
+// parts, U tiles in flight each.  A lane reads the 32 elements of X of its row
+// and block and quantizes them in registers.  The waves' sums meet in LDS in a
+// fixed order.  One row, 4096 -> 4096: 4.5 us, 1.8 of them the launch (8.9 MB); 64
+// rows on 64 experts, 2048 -> 1024: 12 us, 71 MB at 5.9 TB/s.
 // ---------------------------------------------------------------------------
 constexpr int kRowsWaves = 8;
 
