@@ -141,3 +141,21 @@ def test_strides(mx, dtype, F):
     d = torch.zeros(M, F + 5, dtype=dt, device="cuda")[:, 1:1 + F]
     d.copy_(dh)
     assert torch.equal(plan.forward(wide), want[0]) and torch.equal(plan.backward(d), want[1])
+
+
+def test_more_than_one_launch(mx):
+    # over 2^31 pieces of eight columns: the rows go in two launches; compared with a small call on the last rows
+    import torch
+    F = 32
+    M = ((1 << 31) - 256) // 4 + 1000
+    if torch.cuda.mem_get_info()[0] < 160e9:
+        pytest.skip("needs 160 GB of GPU memory")
+    n = 3000
+    x = torch.zeros(M, F, dtype=torch.bfloat16, device="cuda")
+    x[-n:] = torch.randn(n, F, generator=torch.Generator(device="cuda").manual_seed(1), device="cuda").bfloat16()
+    plan, small = mx.ActPlan(M, F, "gelu", False), mx.ActPlan(n, F, "gelu", False)
+    h = plan.forward(x)
+    assert torch.equal(h[-n:], small.forward(x[-n:])) and not h[:4].any()
+    assert torch.equal(plan.codes.view(M, F)[-n:], small.codes.view(n, F))
+    dh = x          # any values
+    assert torch.equal(plan.backward(dh)[-n:], small.backward(x[-n:]))

@@ -497,6 +497,53 @@ def test_graph_replay(mx, M, K, N, E, train):
     assert x2 is not None
 
 
+def test_elements_past_32_bits(mx):
+    # 2.25e9 elements of X and of dX, 1.1e6 rows as an inner axis; compared with small calls on the first and last rows
+    import torch
+    M, K, N, E = 1_100_003, 2048, 48, 3
+    if torch.cuda.mem_get_info()[0] < 40e9:
+        pytest.skip("needs 40 GB of GPU memory")
+    g = torch.Generator(device="cuda").manual_seed(1)
+    x = torch.empty(M, K, dtype=torch.bfloat16, device="cuda")
+    for i in range(0, M, 1 << 17):
+        x[i:i + (1 << 17)].normal_(generator=g)
+    dy = torch.randn(M, N, generator=g, device="cuda").bfloat16()
+    w = torch.randn(N, K, generator=g, device="cuda").bfloat16()
+    a, t = mx.quantize(x, True, True)
+    n = 512
+    codes = a.codes.view(-1)
+    for lo in (0, M - M % 16 - n):      # whole groups of 16 rows
+        part = mx.quantize(x[lo:lo + n])[0]
+        at = lo // 16 * (K // 512) * 4096
+        assert torch.equal(codes[at:at + part.codes.numel()], part.codes.view(-1))
+    lo = M // 512 * 512                 # the last unit of the other axis
+    part = mx.quantize(x[lo:], False, True)[1]
+    per = -(-M // 512) * 4096           # bytes of a group of 16 columns
+    got = t.codes.view(-1, per)[:, -4096:]
+    tiles = -(-(M - lo) // 128)
+    assert torch.equal(got.reshape(-1, 4, 1024)[:, :tiles], part.codes.view(-1, 4, 1024)[:, :tiles])
+
+    plan = mx.LinearPlan(M, K, N)
+    y = plan.forward(x, mx.quantize(w)[0])
+    few = mx.LinearPlan(500, K, N).forward(x[-500:], mx.quantize(w)[0])
+    assert torch.equal(y[-500:].float(), few.float()) or (y[-500:].float() - few.float()).abs().max() <= 2 ** -7 * few.abs().max()
+    del plan, y, t
+
+    # by expert, the input gradient [M, K]
+    wt = torch.randn(E, N, K, generator=g, device="cuda").bfloat16()
+    cut = [0, M - 700, M - 300, M]
+    o = torch.tensor(cut, dtype=torch.int32, device="cuda")
+    d = mx.quantize(dy)[0]
+    b = mx.quantize(wt, False, True)[1]
+    dx = torch.empty(M, K, dtype=torch.bfloat16, device="cuda")
+    mx.sq_mx_gemm_experts(d.codes, d.scales, N, o, E, b.codes, b.scales, dx)
+    dv, bv = mx.quantize(dy[-400:])[0].values().double(), b.values().double()
+    for e, (lo, hi) in ((1, (0, 100)), (2, (100, 400))):
+        want = dv[lo:hi] @ bv[e].T
+        got = dx[M - 400 + lo:M - 400 + hi].double()
+        assert ((got - want).abs() <= (want.abs() + 1e-3) * 2.0 ** -8).all()
+
+
 @pytest.mark.parametrize("M", [1, 16, 5000])
 @pytest.mark.parametrize("K,N", [(0, 70), (1, 1), (70, 0)])
 def test_no_columns(mx, M, K, N):
