@@ -245,8 +245,10 @@ __device__ __forceinline__ void product(const MxProduct& d, uint32_t block, uint
 #pragma unroll
         for (int j = 0; j < T::FN; ++j)
 #pragma unroll
-            for (int i = 0; i < T::FM; ++i)
+            for (int q = 0; q < T::FM; ++q) {
+                const int i = j & 1 ? T::FM - 1 - q : q;
                 acc[i][j] = mfma4<(s & 3)>(fb[buf][j], fa[buf][i], acc[i][j], sb[T::kScalesInLds ? 0 : grp][j], sa[grp][i]);
+            }
     };
     // Step t, of index S in the cycle.
     auto step = [&](int t, auto S) {
