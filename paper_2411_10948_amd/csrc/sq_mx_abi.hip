@@ -444,7 +444,10 @@ sq_status sq_mx_layer_forward(const sq_mx_layer* layer, const void* X, int64_t l
         SQ_TRY(check_product(l.rows, l.c_out, l.c_in, l.experts));
         if (l.rows > 0 && l.c_out > 0) {
             SQ_TRY(check_values(Y, l.type, ldy, l.c_out, "Y"));
-            if (l.c_in > 0) SQ_TRY(check_mx(l.w, l.w_scales, "w"));
+            if (l.c_in > 0) {
+                SQ_TRY(check_mx(l.w, l.w_scales, "w"));
+                SQ_TRY(check_mx(l.x, l.x_scales, "x"));
+            }
         }
         SQ_TRY(check_workspace(l.workspace, l.workspace_bytes, layer_workspace(layer)));
         SQ_TRY(sq_mx_quantize(X, l.type, 1, l.rows, l.c_in, ld, 0, offsets, l.experts, l.x, l.x_scales, l.x_t, l.x_t_scales,
@@ -467,11 +470,17 @@ sq_status sq_mx_layer_backward(const sq_mx_layer* layer, const void* dY, int64_t
         SQ_TRY(check_blocks(l.c_out, 16, l.c_in, 16, 0, std::max<int64_t>(l.experts, 1)));
         if (l.rows > 0 && l.c_in > 0) {
             SQ_TRY(check_values(dX, l.type, ld_dx, l.c_in, "dX"));
-            if (l.c_out > 0) SQ_TRY(check_mx(l.w_t, l.w_t_scales, "w_t"));
+            if (l.c_out > 0) {
+                SQ_TRY(check_mx(l.w_t, l.w_t_scales, "w_t"));
+                SQ_TRY(check_mx(l.dy, l.dy_scales, "dy"));
+            }
         }
         if (l.c_out > 0 && l.c_in > 0) {
             SQ_TRY(check_values(dW, SQ_TYPE_F32, ld_dw, l.c_in, "dW"));
-            if (l.rows > 0) SQ_TRY(check_mx(l.x_t, l.x_t_scales, "x_t"));
+            if (l.rows > 0) {
+                SQ_TRY(check_mx(l.x_t, l.x_t_scales, "x_t"));
+                SQ_TRY(check_mx(l.dy_t, l.dy_t_scales, "dy_t"));
+            }
         }
         SQ_TRY(check_workspace(l.workspace, l.workspace_bytes, layer_workspace(layer)));
         SQ_TRY(sq_mx_quantize(dY, l.type, 1, l.rows, l.c_out, ld, 0, offsets, l.experts, l.dy, l.dy_scales, l.dy_t,

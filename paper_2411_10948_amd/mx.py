@@ -11,6 +11,7 @@ from __future__ import annotations
 
 import ctypes as ct
 import dataclasses
+import functools
 from typing import Optional, Tuple
 
 import torch
@@ -23,6 +24,8 @@ ACT_SILU = 0
 ACT_GELU = 1
 ACT_KINDS = {"silu": ACT_SILU, "gelu": ACT_GELU}
 
+_current_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", lambda gpu: torch.cuda.current_stream(gpu).cuda_stream)
 _TYPES = {torch.float32: TYPE_F32, torch.bfloat16: TYPE_BF16}
 
 
@@ -49,13 +52,33 @@ def _shape(t: torch.Tensor, shape, name: str) -> None:
         raise ValueError(f"{name}: expected shape {tuple(shape)}, got {tuple(t.shape)}")
 
 
-def _offsets(offsets: Optional[torch.Tensor], experts: int) -> Optional[int]:
+def _like(t: torch.Tensor, shape, other: torch.Tensor, name: str) -> None:
+    """Shape as given, type and place of ``other``."""
+    _shape(t, shape, name)
+    if t.dtype != other.dtype or t.device != other.device:
+        raise ValueError(f"{name}: expected {other.dtype} on {other.device}, got {t.dtype} on {t.device}")
+
+
+def _sized(codes: Optional[torch.Tensor], scales: Optional[torch.Tensor], sizes, name: str) -> Tuple[Optional[int], Optional[int]]:
+    """The pointers of codes and scales, which hold at least ``sizes`` bytes."""
+    for t, n in zip((codes, scales), sizes):
+        if t is not None and (not t.is_cuda or t.element_size() != 1 or not t.is_contiguous() or t.numel() < n):
+            raise ValueError(f"{name}: expected {n} contiguous bytes on the GPU")
+    return _ptr(codes), _ptr(scales)
+
+
+def _mx(codes, scales, rows: int, cols: int, name: str, stack: int = 1):
+    nc, ns = _mx_size(rows, cols)
+    return _sized(codes, scales, (nc * stack, ns * stack), name)
+
+
+def _offsets(offsets: Optional[torch.Tensor], experts: int, gpu: Optional[int] = None) -> Optional[int]:
     if offsets is None:
         if experts:
             raise ValueError("offsets: missing")
         return None
     if (offsets.dtype != torch.int32 or offsets.shape != (experts + 1,) or not offsets.is_contiguous()
-            or not offsets.is_cuda):
+            or (not offsets.is_cuda if gpu is None else offsets.get_device() != gpu)):
         raise ValueError(f"offsets: expected {experts + 1} contiguous int32 values on the GPU")
     return offsets.data_ptr()
 
@@ -78,6 +101,8 @@ class MxMatrix:
         for t, size, name in ((self.codes, nc, "codes"), (self.scales, ns, "scales")):
             if t.dtype != torch.uint8 or not t.is_contiguous() or t.numel() < n * size:
                 raise ValueError(f"{name}: expected at least {n * size} contiguous uint8 values")
+        if self.codes.device != self.scales.device:
+            raise ValueError("codes and scales are on different devices")
 
     @classmethod
     def empty(cls, rows: int, cols: int, stack: int = 0, device="cuda") -> "MxMatrix":
@@ -106,6 +131,9 @@ def sq_mx_size(rows: int, cols: int) -> Tuple[int, int]:
     return a.value, b.value
 
 
+_mx_size = functools.lru_cache(maxsize=1024)(sq_mx_size)     # of the arguments alone
+
+
 def sq_mx_segment_cols(rows: int, experts: int) -> int:
     n = _I64(0)
     _check("sq_mx_segment_cols", load().sq_mx_segment_cols(rows, experts, ct.byref(n)))
@@ -122,14 +150,16 @@ def sq_mx_quantize(X, codes, scales, codes_t, scales_t, offsets=None, experts=0,
     else:
         (rows, cols), batch, ld, stride = X.shape, 1, _rows(X, "X"), 0
     _check("sq_mx_quantize", load().sq_mx_quantize(
-        _ptr(X), _type(X), batch, rows, cols, ld, stride, _offsets(offsets, experts), experts, _ptr(codes), _ptr(scales),
-        _ptr(codes_t), _ptr(scales_t), _stream(stream)))
+        _ptr(X), _type(X), batch, rows, cols, ld, stride, _offsets(offsets, experts), experts,
+        *_mx(codes, scales, rows, cols, "codes", batch),
+        *_mx(codes_t, scales_t, cols, sq_mx_segment_cols(rows, experts) if experts else rows, "codes_t", batch),
+        _stream(stream)))
 
 
 def sq_mx_dequantize(codes, scales, rows, cols, out, stream=None) -> None:
     _shape(out, (rows, cols), "out")
     _check("sq_mx_dequantize", load().sq_mx_dequantize(
-        _ptr(codes), _ptr(scales), rows, cols, _ptr(out), _type(out), _rows(out, "out"), _stream(stream)))
+        *_mx(codes, scales, rows, cols, "codes"), rows, cols, _ptr(out), _type(out), _rows(out, "out"), _stream(stream)))
 
 
 def sq_mx_gemm_workspace_size(M: int, N: int, K: int) -> int:
@@ -142,15 +172,15 @@ def sq_mx_gemm(A, A_scales, B, B_scales, K, C, workspace=None, stream=None) -> N
     M, N = C.shape
     ws, nws = _ws_ptr(workspace)
     _check("sq_mx_gemm", load().sq_mx_gemm(
-        _ptr(A), _ptr(A_scales), _ptr(B), _ptr(B_scales), M, N, K, _ptr(C), _type(C), _rows(C, "C"), ws, nws,
+        *_mx(A, A_scales, M, K, "A"), *_mx(B, B_scales, N, K, "B"), M, N, K, _ptr(C), _type(C), _rows(C, "C"), ws, nws,
         _stream(stream)))
 
 
 def sq_mx_gemm_experts(A, A_scales, K, offsets, experts, B, B_scales, C, stream=None) -> None:
     M, N = C.shape
     _check("sq_mx_gemm_experts", load().sq_mx_gemm_experts(
-        _ptr(A), _ptr(A_scales), M, K, _offsets(offsets, experts), experts, _ptr(B), _ptr(B_scales), N, _ptr(C), _type(C),
-        _rows(C, "C"), _stream(stream)))
+        *_mx(A, A_scales, M, K, "A"), M, K, _offsets(offsets, experts), experts, *_mx(B, B_scales, N, K, "B", experts), N,
+        _ptr(C), _type(C), _rows(C, "C"), _stream(stream)))
 
 
 def sq_mx_gemm_experts_wgrad_workspace_size(rows: int, experts: int, M: int, N: int) -> int:
@@ -165,8 +195,10 @@ def sq_mx_gemm_experts_wgrad(A, A_scales, B, B_scales, rows, offsets, experts, C
     if C.dim() != 3 or C.shape[0] != experts or not C.is_contiguous():
         raise ValueError("C: expected a contiguous [experts, M, N] tensor")
     ws, nws = _ws_ptr(workspace)
+    inner = sq_mx_segment_cols(rows, experts)
     _check("sq_mx_gemm_experts_wgrad", load().sq_mx_gemm_experts_wgrad(
-        _ptr(A), _ptr(A_scales), _ptr(B), _ptr(B_scales), rows, _offsets(offsets, experts), experts, C.shape[1], C.shape[2],
+        *_mx(A, A_scales, C.shape[1], inner, "A"), *_mx(B, B_scales, C.shape[2], inner, "B"), rows,
+        _offsets(offsets, experts), experts, C.shape[1], C.shape[2],
         _ptr(C), _type(C), max(C.shape[2], 1), ws, nws, _stream(stream)))
 
 
@@ -179,10 +211,11 @@ def sq_mx_linear_workspace_size(M: int, K: int, N: int, experts: int = 0) -> int
 def sq_mx_linear(X, W, W_scales, Y, workspace=None, offsets=None, experts=0, stream=None) -> None:
     M, K = X.shape
     N = Y.shape[1]
+    _shape(Y, (M, N), "Y")
     ws, nws = _ws_ptr(workspace)
     _check("sq_mx_linear", load().sq_mx_linear(
-        _ptr(X), _type(X), M, K, _rows(X, "X"), _offsets(offsets, experts), experts, _ptr(W), _ptr(W_scales), N, _ptr(Y),
-        _type(Y), _rows(Y, "Y"), ws, nws, _stream(stream)))
+        _ptr(X), _type(X), M, K, _rows(X, "X"), _offsets(offsets, experts), experts,
+        *_mx(W, W_scales, N, K, "W", max(experts, 1)), N, _ptr(Y), _type(Y), _rows(Y, "Y"), ws, nws, _stream(stream)))
 
 
 class Layer(ct.Structure):
@@ -198,26 +231,44 @@ def sq_mx_layer_workspace_size(layer: Layer) -> int:
     return nb.value
 
 
+def _of_layer(layer: Layer, t: torch.Tensor, shape, name: str, type_=None) -> int:
+    """The pointer of a tensor of the layer's type (or ``type_``) and that shape."""
+    _shape(t, shape, name)
+    if _type(t) != (layer.type if type_ is None else type_):
+        raise TypeError(f"{name}: {t.dtype} is not its type in the layer")
+    return t.data_ptr()
+
+
+def _layer_stack(layer: Layer) -> Tuple[int, ...]:
+    one = (layer.c_out, layer.c_in)
+    return (layer.experts, *one) if layer.experts else one
+
+
 def sq_mx_layer_weight(layer: Layer, W, stream=None) -> None:
     """W [c_out, c_in], or [experts, c_out, c_in]"""
+    w = _of_layer(layer, W, _layer_stack(layer), "W")
     st = W.stride()
     if st[-1] != 1 and W.shape[-1] > 1:
         raise ValueError("W: expected unit column stride")
     ld = st[-2] if W.shape[-2] > 1 else max(st[-2], W.shape[-1])
-    _check("sq_mx_layer_weight", load().sq_mx_layer_weight(ct.addressof(layer), W.data_ptr(), ld, st[0], _stream(stream)))
+    _check("sq_mx_layer_weight", load().sq_mx_layer_weight(ct.addressof(layer), w, ld, st[0], _stream(stream)))
 
 
 def sq_mx_layer_forward(layer: Layer, X, offsets, Y, stream=None) -> None:
     _check("sq_mx_layer_forward", load().sq_mx_layer_forward(
-        ct.addressof(layer), X.data_ptr(), _rows(X, "X"), None if offsets is None else offsets.data_ptr(), Y.data_ptr(),
-        _rows(Y, "Y"), _stream(stream)))
+        ct.addressof(layer), _of_layer(layer, X, (layer.rows, layer.c_in), "X"), _rows(X, "X"),
+        _offsets(offsets, layer.experts), _of_layer(layer, Y, (layer.rows, layer.c_out), "Y"), _rows(Y, "Y"),
+        _stream(stream)))
 
 
 def sq_mx_layer_backward(layer: Layer, dY, offsets, dX, dW, stream=None) -> None:
     """dW [c_out, c_in] or [experts, c_out, c_in], contiguous"""
+    if not dW.is_contiguous():
+        raise ValueError("dW: expected a contiguous tensor")
     _check("sq_mx_layer_backward", load().sq_mx_layer_backward(
-        ct.addressof(layer), dY.data_ptr(), _rows(dY, "dY"), None if offsets is None else offsets.data_ptr(), dX.data_ptr(),
-        _rows(dX, "dX"), dW.data_ptr(), max(dW.shape[-1], 1), _stream(stream)))
+        ct.addressof(layer), _of_layer(layer, dY, (layer.rows, layer.c_out), "dY"), _rows(dY, "dY"),
+        _offsets(offsets, layer.experts), _of_layer(layer, dX, (layer.rows, layer.c_in), "dX"), _rows(dX, "dX"),
+        _of_layer(layer, dW, _layer_stack(layer), "dW", TYPE_F32), max(layer.c_in, 1), _stream(stream)))
 
 
 def sq_act_size(M: int, F: int, gated: bool) -> Tuple[int, int]:
@@ -228,16 +279,18 @@ def sq_act_size(M: int, F: int, gated: bool) -> Tuple[int, int]:
 
 def sq_act_forward(X, kind, gated, H, codes, scales, stream=None) -> None:
     M, F = H.shape
+    _like(X, (M, 2 * F if gated else F), H, "X")
     _check("sq_act_forward", load().sq_act_forward(
-        _ptr(X), _type(X), kind, int(gated), M, F, _rows(X, "X"), _ptr(H), _rows(H, "H"), _ptr(codes), _ptr(scales),
-        _stream(stream)))
+        _ptr(X), _type(X), kind, int(gated), M, F, _rows(X, "X"), _ptr(H), _rows(H, "H"),
+        *_sized(codes, scales, sq_act_size(M, F, gated), "codes"), _stream(stream)))
 
 
 def sq_act_backward(dH, kind, gated, codes, scales, dX, stream=None) -> None:
     M, F = dH.shape
+    _like(dX, (M, 2 * F if gated else F), dH, "dX")
     _check("sq_act_backward", load().sq_act_backward(
-        _ptr(dH), _type(dH), kind, int(gated), M, F, _rows(dH, "dH"), _ptr(codes), _ptr(scales), _ptr(dX), _rows(dX, "dX"),
-        _stream(stream)))
+        _ptr(dH), _type(dH), kind, int(gated), M, F, _rows(dH, "dH"),
+        *_sized(codes, scales, sq_act_size(M, F, gated), "codes"), _ptr(dX), _rows(dX, "dX"), _stream(stream)))
 
 
 # ---------------------------------------------------------------------------
@@ -265,18 +318,30 @@ def quantize(X: torch.Tensor, rows: bool = True, cols: bool = False, offsets: Op
 # layers (a token through 4096 x 4096: 6.4 us a call through the wrappers above,
 # 4.5 us on the GPU): an input is looked at once, and what does not change from
 # call to call is kept as integers.
-def _checked(t: torch.Tensor, shape, dtype, name: str) -> int:
+def _checked(t: torch.Tensor, shape, dtype, gpu: int, name: str) -> int:
     """The row stride of a plan's input, after a look at its shape, type, place and strides."""
     if t.shape != shape:
         raise ValueError(f"{name}: expected shape {tuple(shape)}, got {tuple(t.shape)}")
     if t.dtype is not dtype:
         raise TypeError(f"{name}: expected {dtype}, got {t.dtype}")
-    if not t.is_cuda:
-        raise ValueError(f"{name}: expected a tensor on the GPU")
+    if t.get_device() != gpu:
+        raise ValueError(f"{name}: expected a tensor on the plan's GPU, got one on {t.device}")
     st = t.stride()
     if st[-1] != 1 and shape[-1] > 1:
         raise ValueError(f"{name}: expected unit column stride")
     return st[-2] if shape[-2] > 1 else max(st[-2], shape[-1])
+
+
+def _gpu_of(t: torch.Tensor) -> int:
+    """Index of the GPU of a plan's buffer; no tensor has that of a plan elsewhere."""
+    return t.get_device() if t.is_cuda else -2
+
+
+def _on(gpu: int, stream) -> int:
+    """The stream of a plan's launches, which go to the current GPU."""
+    if _current_device() != gpu:
+        raise ValueError("the plan's GPU is not the current one")
+    return _raw_stream(gpu) if stream is None else stream.cuda_stream
 
 
 class LinearPlan:
@@ -301,7 +366,8 @@ class LinearPlan:
         self._w_shape = torch.Size((experts, C_out, C_in) if experts else (C_out, C_in))
         self.Y = torch.empty(self._y_shape, dtype=dtype, device=dev)
         self.offsets, self._off_ptr, self._type = None, None, _TYPES[dtype]
-        self._y_ptr, self._y_ld, self._lib = self.Y.data_ptr(), max(C_out, 1), load()
+        self._y_ptr, self._y_ld, self._lib, self._gpu = self.Y.data_ptr(), max(C_out, 1), load(), _gpu_of(self.Y)
+        self._has_weight = self._has_input = False
         if not train:
             self.ws = _workspace(sq_mx_linear_workspace_size(M, C_in, C_out, experts), dev)
             self._ws = _ws_ptr(self.ws)
@@ -332,41 +398,52 @@ class LinearPlan:
         """W [C_out, C_in], or [experts, C_out, C_in]"""
         if not self.train:
             raise ValueError("quantize_weight needs a plan with train=True")
-        ld = _checked(W, self._w_shape, self.dtype, "W")
-        _check("sq_mx_layer_weight", self._lib.sq_mx_layer_weight(
-            self._layer_ptr, W.data_ptr(), ld, W.stride(0), _stream(stream)))
+        ld = _checked(W, self._w_shape, self.dtype, self._gpu, "W")
+        st = self._lib.sq_mx_layer_weight(
+            self._layer_ptr, W.data_ptr(), ld, W.stride(0), _on(self._gpu, stream))
+        if st:
+            _check("sq_mx_layer_weight", st)
+        self._has_weight = True
 
     def forward(self, x: torch.Tensor, w: Optional[MxMatrix] = None, offsets: Optional[torch.Tensor] = None, stream=None):
-        ld = _checked(x, self._x_shape, self.dtype, "x")
-        off = _offsets(offsets, self.experts)
+        ld = _checked(x, self._x_shape, self.dtype, self._gpu, "x")
+        off = _offsets(offsets, self.experts, self._gpu)
         if self.train:
             if w is not None:
                 raise ValueError("w: a training plan has its own codes (quantize_weight)")
-            self.offsets, self._off_ptr = offsets, off
-            _check("sq_mx_layer_forward", self._lib.sq_mx_layer_forward(
-                self._layer_ptr, x.data_ptr(), ld, off, self._y_ptr, self._y_ld, _stream(stream)))
+            if not self._has_weight:
+                raise ValueError("forward needs a quantize_weight before it")
+            st = self._lib.sq_mx_layer_forward(
+                self._layer_ptr, x.data_ptr(), ld, off, self._y_ptr, self._y_ld, _on(self._gpu, stream))
+            if st:
+                _check("sq_mx_layer_forward", st)
+            self.offsets, self._off_ptr, self._has_input = offsets, off, True
             return self.Y
         if w is None or w.rows != self.C_out or w.cols != self.C_in or (w.stack or 1) != (self.experts or 1):
             raise ValueError(f"w: expected codes of {self.experts or 'one'} [{self.C_out}, {self.C_in}]")
         codes = w.codes
-        if not codes.is_cuda:
-            raise ValueError("w: expected codes on the GPU")
+        if codes.get_device() != self._gpu:
+            raise ValueError("w: expected codes on the plan's GPU")
         t = self._type
-        _check("sq_mx_linear", self._lib.sq_mx_linear(
+        st = self._lib.sq_mx_linear(
             x.data_ptr(), t, self.M, self.C_in, ld, off, self.experts, codes.data_ptr(), w.scales.data_ptr(), self.C_out,
-            self._y_ptr, t, self._y_ld, *self._ws, _stream(stream)))
+            self._y_ptr, t, self._y_ld, *self._ws, _on(self._gpu, stream))
+        if st:
+            _check("sq_mx_linear", st)
         return self.Y
 
     def backward(self, dy: torch.Tensor, stream=None):
         """(dX, dW) of the last forward"""
         if not self.train:
             raise ValueError("backward needs a plan with train=True")
-        ld = _checked(dy, self._y_shape, self.dtype, "dy")
-        if self.experts and self.offsets is None:
+        ld = _checked(dy, self._y_shape, self.dtype, self._gpu, "dy")
+        if not self._has_input:
             raise ValueError("backward needs a forward before it")
-        _check("sq_mx_layer_backward", self._lib.sq_mx_layer_backward(
+        st = self._lib.sq_mx_layer_backward(
             self._layer_ptr, dy.data_ptr(), ld, self._off_ptr, self._dx_ptr, self._dw_ld, self._dw_ptr, self._dw_ld,
-            _stream(stream)))
+            _on(self._gpu, stream))
+        if st:
+            _check("sq_mx_layer_backward", st)
         return self.dX, self.dW
 
 
@@ -389,22 +466,31 @@ class ActPlan:
         self._h_shape, self._x_shape = torch.Size((M, F)), torch.Size((M, self.width))
         self.H = torch.empty(self._h_shape, dtype=dtype, device=dev)
         self.dX = torch.empty(self._x_shape, dtype=dtype, device=dev)
-        self._lib, self._type, self._gated = load(), _TYPES[dtype], int(gated)
+        self._lib, self._type, self._gated, self._gpu = load(), _TYPES[dtype], int(gated), _gpu_of(self.H)
+        self._has_input = False
         self._held = (self.codes, self.scales, self.H, self.dX)     # what _ptrs point at
         self._ptrs = tuple(t.data_ptr() for t in self._held)
         self._h_ld, self._x_ld = max(F, 1), max(self.width, 1)
 
     def forward(self, x: torch.Tensor, stream=None) -> torch.Tensor:
-        ld = _checked(x, self._x_shape, self.dtype, "x")
+        ld = _checked(x, self._x_shape, self.dtype, self._gpu, "x")
         codes, scales, h, _ = self._ptrs
-        _check("sq_act_forward", self._lib.sq_act_forward(
-            x.data_ptr(), self._type, self.kind, self._gated, self.M, self.F, ld, h, self._h_ld, codes, scales, _stream(stream)))
+        st = self._lib.sq_act_forward(
+            x.data_ptr(), self._type, self.kind, self._gated, self.M, self.F, ld, h, self._h_ld, codes, scales,
+            _on(self._gpu, stream))
+        if st:
+            _check("sq_act_forward", st)
+        self._has_input = True
         return self.H
 
     def backward(self, dh: torch.Tensor, stream=None) -> torch.Tensor:
-        ld = _checked(dh, self._h_shape, self.dtype, "dh")
+        ld = _checked(dh, self._h_shape, self.dtype, self._gpu, "dh")
+        if not self._has_input:
+            raise ValueError("backward needs a forward before it")
         codes, scales, _, dx = self._ptrs
-        _check("sq_act_backward", self._lib.sq_act_backward(
+        st = self._lib.sq_act_backward(
             dh.data_ptr(), self._type, self.kind, self._gated, self.M, self.F, ld, codes, scales, dx, self._x_ld,
-            _stream(stream)))
+            _on(self._gpu, stream))
+        if st:
+            _check("sq_act_backward", st)
         return self.dX

@@ -568,3 +568,67 @@ def test_empty(mx):
     plan.dW.fill_(3.0)
     plan.forward(torch.empty(0, 64, device="cuda"), offsets=torch.zeros(4, dtype=torch.int32, device="cuda"))
     assert not plan.backward(torch.empty(0, 32, device="cuda"))[1].any()
+
+
+def test_refusals_on_the_gpu(mx):
+    import torch
+    plan = mx.LinearPlan(32, 64, 48, train=True)
+    x, dy = torch.zeros(32, 64, dtype=torch.bfloat16, device="cuda"), torch.zeros(32, 48, dtype=torch.bfloat16, device="cuda")
+    with pytest.raises(ValueError, match="quantize_weight"):
+        plan.forward(x)
+    plan.quantize_weight(torch.zeros(48, 64, dtype=torch.bfloat16, device="cuda"))
+    with pytest.raises(ValueError, match="forward"):
+        plan.backward(dy)
+    with pytest.raises(ValueError, match="forward"):
+        mx.ActPlan(32, 48, gated=False).backward(dy)
+    with pytest.raises(ValueError, match="GPU"):
+        plan.forward(x.cpu())
+    with pytest.raises(TypeError):
+        plan.forward(x.float())
+    with pytest.raises(ValueError):
+        plan.forward(x.t().contiguous().t())        # rows that are not contiguous
+    a, w = mx.quantize(x)[0], mx.quantize(torch.zeros(48, 64, dtype=torch.bfloat16, device="cuda"))[0]
+    y = torch.empty(32, 48, device="cuda")
+    with pytest.raises(ValueError, match="B:"):
+        mx.sq_mx_gemm(a.codes, a.scales, w.codes.view(-1)[:-16], w.scales, 64, y)
+    with pytest.raises(ValueError, match="A:"):
+        mx.sq_mx_gemm(a.codes, a.scales, w.codes, w.scales, 64, torch.empty(33, 48, device="cuda"))
+    with pytest.raises(ValueError, match="B:"):
+        o = torch.tensor([0, 16, 32], dtype=torch.int32, device="cuda")
+        mx.sq_mx_gemm_experts(a.codes, a.scales, 64, o, 2, w.codes, w.scales, y)     # codes of one expert
+    with pytest.raises(ValueError, match="codes_t:"):
+        t = mx.MxMatrix.empty(64, 32)
+        mx.sq_mx_quantize(x, None, None, t.codes, t.scales, torch.tensor([0, 16, 32], dtype=torch.int32, device="cuda"), 2)
+    with pytest.raises(ValueError, match="X:"):
+        h = torch.empty(32, 64, dtype=torch.bfloat16, device="cuda")
+        mx.sq_act_forward(x, mx.ACT_SILU, True, h, a.codes, a.scales)
+    torch.cuda.synchronize()
+
+
+@pytest.mark.parametrize("E", [0, 3])
+def test_layer_calls_one_by_one(mx, E):
+    # the wrappers of the layer's three steps give what the plan gives, and refuse what does not fit the layer
+    import torch
+    M, K, N = 70, 96, 40
+    rng = np.random.default_rng(3)
+    x, _ = _rand(rng, (M, K), "bf16")
+    dy, _ = _rand(rng, (M, N), "bf16")
+    w, _ = _rand(rng, (E, N, K) if E else (N, K), "bf16")
+    o = torch.tensor([0, 13, 13, 70], dtype=torch.int32, device="cuda") if E else None
+    plan, other = (mx.LinearPlan(M, K, N, experts=E, train=True) for _ in range(2))
+    plan.quantize_weight(w)
+    want = plan.forward(x, offsets=o), *plan.backward(dy)
+    y, dx, dw = (torch.empty_like(t) for t in want)
+    mx.sq_mx_layer_weight(other.layer, w)
+    mx.sq_mx_layer_forward(other.layer, x, o, y)
+    mx.sq_mx_layer_backward(other.layer, dy, o, dx, dw)
+    for a, b in zip(want, (y, dx, dw)):
+        assert torch.equal(a, b)
+    with pytest.raises(ValueError, match="X:"):
+        mx.sq_mx_layer_forward(other.layer, x[:-1], o, y)
+    with pytest.raises(TypeError, match="W:"):
+        mx.sq_mx_layer_weight(other.layer, w.float())
+    with pytest.raises(TypeError, match="dW:"):
+        mx.sq_mx_layer_backward(other.layer, dy, o, dx, dw.bfloat16())
+    with pytest.raises(ValueError, match="offsets"):
+        mx.sq_mx_layer_forward(other.layer, x, o[:-1] if E else torch.zeros(1, dtype=torch.int32, device="cuda")[:0], y)

@@ -199,3 +199,35 @@ def test_binding_refusals(mx):
         plan.forward(x, w, torch.zeros(4, dtype=torch.int32))       # tensors that are not on the GPU
     with pytest.raises(ValueError):
         plan.backward(torch.zeros(4, 6))
+
+
+def test_refusals_of_layer_buffers(mx):
+    """Codes that one of the two products reads and the other does not."""
+    from paper_2411_10948_amd.mx import Layer
+    from paper_2411_10948_amd.shiftquant import load
+    L, p = load(), ct.c_void_p(0x100000)        # never read: every call is refused
+    sizes = dict(rows=256, c_in=64, c_out=64, experts=0, type=0, reserved=0, workspace_bytes=1 << 40)
+    for name in ("x", "dy", "x_t", "dy_t", "w", "w_t"):
+        for field in (name, name + "_scales"):
+            for bad in (None, 0x100002):
+                layer = Layer(*({**{f[0]: 0x100000 for f in Layer._fields_}, **sizes, field: bad}[f[0]] for f in Layer._fields_))
+                if name in ("x", "w"):
+                    assert L.sq_mx_layer_forward(ct.byref(layer), p, 64, None, p, 64, None) == 1
+                else:
+                    assert L.sq_mx_layer_backward(ct.byref(layer), p, 64, None, p, 64, p, 64, None) == 1
+
+
+def test_refusals_of_places_and_sizes(mx):
+    import torch
+    b = lambda n: torch.empty(n, dtype=torch.uint8)
+    nc, ns = mx.sq_mx_size(16, 512)
+    out = torch.empty(16, 16)
+    with pytest.raises(ValueError, match="on the GPU"):
+        mx.sq_mx_gemm(b(nc), b(ns), b(nc), b(ns), 512, out)
+    with pytest.raises(ValueError, match="on the GPU"):
+        mx.sq_mx_dequantize(b(nc), b(ns), 16, 512, torch.empty(16, 512))
+    with pytest.raises(ValueError, match="H|X"):
+        mx.sq_act_forward(torch.empty(4, 64), mx.ACT_SILU, True, torch.empty(4, 64), b(512), b(16))
+    plan = mx.LinearPlan(4, 8, 6, dtype=torch.float32, device="cpu")
+    with pytest.raises(ValueError, match="GPU"):
+        plan.forward(torch.zeros(4, 8), mx.MxMatrix.empty(6, 8, 0, "cpu"))
