@@ -178,6 +178,33 @@ __device__ __forceinline__ Segment find_segment(const int32_t* offsets, int expe
     }
     return r;
 }
+// find_segment(index_of(tiles of all experts)); none for a negative index.  Up to
+// 64 experts take one look at the offsets.
+template <class F>
+__device__ __forceinline__ Segment find_segment_of(const int32_t* offsets, int experts, int rows, int unit, F index_of) {
+    const int lane = threadIdx.x & 63;
+    int lo, hi;
+    segment_of(offsets, experts, rows, lane, lo, hi);
+    const int t = (hi - lo + unit - 1) / unit, ti = wave_scan(t), first = __builtin_amdgcn_readlane(ti, 63);
+    int total = first;
+    for (int base = 64; base < experts; base += 64) {
+        int l, h;
+        segment_of(offsets, experts, rows, base + lane, l, h);
+        total += __builtin_amdgcn_readlane(wave_scan((h - l + unit - 1) / unit), 63);
+    }
+    const int index = index_of(total);
+    Segment r;
+    if (index < 0) return r;
+    if (index >= first) return find_segment(offsets, experts, rows, unit, index);
+    const uint64_t hit = __ballot(index >= ti - t && index < ti);
+    if (!hit) return r;
+    const int src = __ffsll((unsigned long long)hit) - 1;
+    r.expert = src;
+    r.lo = __builtin_amdgcn_readlane(lo, src);
+    r.hi = __builtin_amdgcn_readlane(hi, src);
+    r.tile = index - __builtin_amdgcn_readlane(ti - t, src);
+    return r;
+}
 // Inner elements before expert e in a segmented transpose, and its rows.
 __device__ __forceinline__ void segment_inner(const int32_t* offsets, int experts, int rows, int e, int64_t& inner,
                                               int& len) {

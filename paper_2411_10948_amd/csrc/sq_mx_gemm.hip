@@ -116,12 +116,16 @@ __device__ __forceinline__ void product(const MxProduct& d, uint32_t block, uint
     const int wm = wave / T::WN, wn = wave % T::WN;
 
     // ---- which product, which tile, which tiles of the inner axis ----
-    uint32_t item = xcd_item(block, d.blocks);
     int64_t expert = 0, split = 0;
     int64_t row_end = p.M, t0 = 0, n_tiles = (p.K + kMxTile - 1) / kMxTile;
+    uint32_t item = 0;
+    if constexpr (MODE == kDense) item = xcd_item(block, d.blocks);
     if constexpr (MODE == kExpertInner) {
-        const uint32_t e = item / (tiles_m * tiles_n);
-        item -= e * tiles_m * tiles_n;
+        // Every expert over all the XCDs: with whole experts on each, the one with
+        // most rows sets the time (gradients of 20000 rows, 8 uneven experts, 1200 x
+        // 3000, 173 -> 150 us; 32768 rows, 16 rather even ones, 2048 x 4096, 411 -> 418).
+        const uint32_t e = block / (tiles_m * tiles_n);
+        item = xcd_item(block - e * tiles_m * tiles_n, tiles_m * tiles_n);
         expert = e;
         int64_t inner;
         int len;
@@ -138,17 +142,28 @@ __device__ __forceinline__ void product(const MxProduct& d, uint32_t block, uint
         n_tiles = min(per, n_tiles - t0);
     }
     // kGroupM tile rows at a time, so that an XCD's blocks share panels of B in its L2
-    const uint32_t per_group = kGroupM * tiles_n, grp0 = item / per_group, first = grp0 * kGroupM;
-    const uint32_t gsz = min(tiles_m - first, kGroupM), u = item - grp0 * per_group, un = u / gsz, tm = first + u - un * gsz;
-    int64_t m0 = (int64_t)tm * T::BM;
-    const int64_t n0 = (int64_t)un * T::BN;
+    uint32_t un = 0;
+    auto tile_row = [&](uint32_t it, uint32_t rows) {
+        const uint32_t per_group = kGroupM * tiles_n, grp0 = it / per_group, first = grp0 * kGroupM;
+        const uint32_t gsz = min(rows - first, kGroupM), u = it - grp0 * per_group;
+        un = u / gsz;
+        return first + u - un * gsz;
+    };
+    int64_t m0 = 0;
+    if constexpr (MODE != kExpertRows) m0 = (int64_t)tile_row(item, tiles_m) * T::BM;
     if constexpr (MODE == kExpertRows) {
-        const Segment g = find_segment(p.offsets, p.experts, (int)p.M, T::BM, (int)tm);
+        // The grid has room for any split of the rows; the tiles that there are go
+        // evenly over the XCDs (16384 rows, 64 experts, 2048 -> 1408: 53 -> 47 us).
+        const Segment g = find_segment_of(p.offsets, p.experts, (int)p.M, T::BM, [&](int rows) {
+            const uint32_t n = (uint32_t)rows * tiles_n;
+            return rows > 0 && block < n ? (int)tile_row(xcd_item(block, n), (uint32_t)rows) : -1;
+        });
         if (g.expert < 0) return;
         expert = g.expert;
         m0 = (int64_t)g.lo + (int64_t)g.tile * T::BM;
         row_end = g.hi;
     }
+    const int64_t n0 = (int64_t)un * T::BN;
 
     // ---- operand loads: a fixed offset per lane, the group and the inner axis in a scalar ----
     // Group g of a stage: rows 16 g.. of A (g < BM / 16), then of B; groups
