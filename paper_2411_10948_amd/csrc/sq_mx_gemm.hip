@@ -591,6 +591,20 @@ __global__ __launch_bounds__(64 * kRowsWaves, 4) void k_mx_rows(MxRowsArgs p, ui
 #endif
 }
 
+// Rows and columns of 128 x 128 tiles (of every expert) and the steps of 128
+// inner elements of each.
+struct MxExtent {
+    int64_t rows, cols, steps;
+};
+MxExtent extent(const MxGemmArgs& a) {
+    MxExtent x;
+    x.rows = a.mode == kExpertRows ? a.M / 128 + std::min<int64_t>(a.experts, a.M) : (a.M + 127) / 128;
+    if (a.mode == kExpertInner) x.rows *= a.experts;
+    x.cols = (a.N + 127) / 128;
+    x.steps = ((a.mode == kExpertInner ? a.rows / a.experts : a.K) + kMxTile - 1) / kMxTile;
+    return x;
+}
+
 enum MxTileKind { kWide, kMid, kShort, kSmall };
 
 // Tiles by the size of the product, each rule with the times in us of the
@@ -604,13 +618,11 @@ enum MxTileKind { kWide, kMid, kShort, kSmall };
 //   Short up to 8 steps: 8192 x 8192 x 512 short 35.4, mid 37.1;
 //     1024 x 8192 x 2048 (16 steps) 16.2 and 15.5.
 MxTileKind tile_kind(const MxGemmArgs& a) {
-    const int64_t times = a.mode == kExpertInner ? a.experts : 1;
-    const int64_t tm = a.mode == kExpertRows ? a.M / 128 + std::min<int64_t>(a.experts, a.M) : (a.M + 127) / 128;
-    if (tm * ((a.N + 127) / 128) * times < 240) return kSmall;
-    const int64_t k = a.mode == kExpertInner ? a.rows / a.experts : a.K, steps = (k + kMxTile - 1) / kMxTile;
-    const int64_t tn = (a.N + 255) / 256, wide = tm * tn * times, rounds = (wide + 255) / 256;
-    if (steps >= 12 && 20 * 256 * tn <= 21 * a.N && 100 * 256 * rounds <= 135 * wide) return kWide;
-    return steps <= 8 ? kShort : kMid;
+    const MxExtent x = extent(a);
+    if (x.rows * x.cols < 240) return kSmall;
+    const int64_t tn = (a.N + 255) / 256, wide = x.rows * tn, rounds = (wide + 255) / 256;
+    if (x.steps >= 12 && 20 * 256 * tn <= 21 * a.N && 100 * 256 * rounds <= 135 * wide) return kWide;
+    return x.steps <= 8 ? kShort : kMid;
 }
 
 template <class T, int MODE>
@@ -661,13 +673,14 @@ hipError_t pair(const MxGemmArgs& a, const MxGemmArgs& b, hipStream_t s) {
 
 }  // namespace
 
-// Few tiles of a long inner axis are split, in parts of at least 24 steps
-// (64 x 64 x 65536 74 us unsplit; 768 x 768 x 3152, 25 steps, 6 us unsplit
-// and 10 with a second launch for the sums).
+// Few tiles of a long inner axis are split, in parts of at least 40 steps: 64 x
+// 640 x 30000, 235 steps, 26.7 us unsplit and 13.3 in 5; 1024 x 1024 x 32768,
+// 256 steps, 42.0 and 35.5 in 2; but 128 x 4096 x 8192, 64 steps, 10.4 and 12.6
+// in 2, 768 x 768 x 3152, 25 steps, 8.9 and 12.6 (a second launch for the sums).
 int64_t mx_gemm_splits(const MxGemmArgs& a) {
     if (a.mode != kDense) return 1;
     const int64_t tiles = ((a.M + 63) / 64) * ((a.N + 63) / 64), k = (a.K + kMxTile - 1) / kMxTile;
-    return std::max<int64_t>(1, std::min<int64_t>(512 / std::max<int64_t>(tiles, 1), k / 24));
+    return std::max<int64_t>(1, std::min<int64_t>(512 / std::max<int64_t>(tiles, 1), k / 40));
 }
 
 namespace {
@@ -701,12 +714,32 @@ hipError_t launch_mx_gemm(const MxGemmArgs& a, hipStream_t s) {
     }
 }
 
+namespace {
+
+// Whether a block of `few` in 128 x 128 tiles, 0.4 us a step, would take longer
+// than both products together: 1.2 ns a tile and step, outputs at 5 TB/s.  In us,
+// gradients in large tiles and in small ones: 16200 x 768 x 1408 82 and 50, 4000
+// x 768 x 1024 28 and 17, 300 x 8192 x 1024 43 and 22 (few blocks that last); 32768 x
+// 1408 x 2048 140 and 196, 6000 x 1500 x 1500 38 and 42, 1187 x 520 x 1000 on 12
+// experts 17.0 and 19.7 (blocks that the rest covers).
+bool outlasts(const MxGemmArgs& few, const MxGemmArgs& other) {
+    const auto rest = [](const MxGemmArgs& a) {
+        const MxExtent x = extent(a);
+        const double bytes = (a.mode == kExpertInner ? (double)a.experts : 1.0) * (double)a.M * (double)a.N *
+                             (a.type == SQ_TYPE_F32 ? 4.0 : 2.0);
+        return 1.2e-3 * (double)(x.rows * x.cols * x.steps) + bytes / 5e6;
+    };
+    return 0.4 * (double)extent(few).steps / (double)mx_gemm_splits(few) > rest(few) + rest(other);
+}
+
+}  // namespace
+
 hipError_t launch_mx_gemm_pair(const MxGemmArgs& a, const MxGemmArgs& b, hipStream_t s) {
     MxTileKind ka = tile_kind(a), kb = tile_kind(b);
-    // A product of few tiles goes along in the other one's: 1187 rows on 12
-    // experts, 520 x 1000, dX in 64 x 64 tiles 5.9 us and dW in 128 x 128 9.9.
-    if (ka == kSmall) ka = kb;
-    if (kb == kSmall) kb = ka;
+    // A product of few tiles goes along in the other one's larger tiles, unless a
+    // block of it would outlast the rest: then both take small tiles.
+    if (ka == kSmall) ka = outlasts(a, b) ? (kb = kSmall) : kb;
+    else if (kb == kSmall) kb = outlasts(b, a) ? (ka = kSmall) : ka;
     if (ka != kb || a.M == 0 || a.N == 0 || b.M == 0 || b.N == 0) {
         const hipError_t e = launch_mx_gemm(a, s);
         return e == hipSuccess ? launch_mx_gemm(b, s) : e;

@@ -161,7 +161,7 @@ def test_quantize_by_expert(mx, name, dtype):
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("M,N,K", [(1, 1, 1), (1, 17, 128), (16, 16, 32), (17, 33, 129), (64, 64, 512), (65, 100, 640),
                                    (100, 130, 1000), (128, 256, 384), (200, 64, 8192), (300, 260, 2100), (33, 1000, 4096),
-                                   (520, 500, 260)])
+                                   (520, 500, 260), (70, 130, 11000), (16, 16, 20500)])
 def test_gemm(mx, M, N, K, dtype):
     import torch
     rng = np.random.default_rng(M + 7 * N + 13 * K)
@@ -196,7 +196,10 @@ def test_gemm_of_many_tiles(mx, M, N, K):
     (4096, 2048, 4096, 0),      # 128 x 256 tiles, both gradients in one launch
     (2000, 1300, 2100, 0),      # 128 x 128, 11 steps
     (2300, 700, 2050, 0),       # 128 x 128, 6 steps; ragged in every direction
-    (4500, 65, 70, 0),          # few tiles of a long inner axis: split
+    (4500, 65, 70, 0),          # few tiles of a long inner axis
+    (14000, 65, 70, 0),         # the same, split
+    (15000, 1030, 260, 0), (300, 520, 8200, 0), (6000, 300, 400, 5),    # one gradient's blocks would outlast the other's
+    (2600, 4100, 130, 0),       # and would not
     (6400, 2048, 2048, 3), (9000, 1300, 1300, 6), (6000, 1000, 1000, 8), (3000, 1700, 2048, 3), (700, 200, 150, 3)])
 def test_training_step_of_every_tile_shape(mx, M, K, N, E):
     # against fp64 products of the values that the step's own codes stand for (the quantizer's tests check those)
@@ -235,11 +238,12 @@ def test_training_step_of_every_tile_shape(mx, M, K, N, E):
         close(dw[e] if E else dw, a, b, hi - lo)
 
 
-@pytest.mark.parametrize("dtype", ["f32", "bf16"])
-def test_quantize_large_inputs(mx, dtype):
-    # inputs of 32 MB and more are read past the last-level cache; compared with the same rows in smaller pieces
+@pytest.mark.parametrize("dtype,C", [("f32", 2049), ("f32", 2080), ("bf16", 4097), ("bf16", 4160)])
+def test_quantize_large_inputs(mx, dtype, C):
+    # inputs of 32 MB and more whose rows are whole lines are read past the last-level cache; compared with the same
+    # rows in smaller pieces
     import torch
-    M, C = 4224, 4097 if dtype == "bf16" else 2049
+    M = 4224
     x = torch.randn(M, C, generator=torch.Generator(device="cuda").manual_seed(1), device="cuda").to(_dtype(dtype))
     a, t = mx.quantize(x, True, True)
     a, t = a.values(), t.values()
