@@ -297,6 +297,18 @@ def test_linear_forward(mx, M, K, N, dtype):
     _close(y.double().cpu().numpy(), want, mag, K, dtype)
 
 
+@pytest.mark.parametrize("shift,pad", [(0, 0), (1, 0), (1, 1), (3, 2)])
+@pytest.mark.parametrize("M,K", [(1, 1), (1, 127), (2, 128), (9, 129), (16, 577), (5, 2050), (1, 4095)])
+def test_few_rows_at_any_address(mx, M, K, shift, pad):
+    import torch
+    rng = np.random.default_rng(K + shift)
+    big, _ = _rand(rng, (M, K + shift + pad), "bf16")
+    x = big[:, shift:shift + K]
+    w, wv = _rand(rng, (70, K), "bf16")
+    want, mag = ref.mx_product(ref.mx_values(x.double().cpu().numpy()), ref.mx_values(wv))
+    _close(mx.LinearPlan(M, K, 70).forward(x, mx.quantize(w)[0]).double().cpu().numpy(), want, mag, K, "bf16")
+
+
 def test_linear_strided_input(mx):
     rng = np.random.default_rng(3)
     for M in (3, 50):
