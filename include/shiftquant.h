@@ -774,8 +774,8 @@ sq_status sq_mx_gemm_experts_wgrad(const uint8_t* A, const uint8_t* A_scales, co
  * sq_mx_linear -- Y [M, N] = X W^T with X [M, K] in fp32 or bf16, quantized on the
  * way: what sq_mx_quantize and sq_mx_gemm (offsets NULL, experts 0) or
  * sq_mx_gemm_experts give.  Few rows (at most 16, or 16 an expert on average;
- * more for small layers) take one launch and no workspace, the serving form
- * for single tokens.
+ * more for small layers, fewer for wide ones of a short inner axis) take one
+ * launch and no workspace, the serving form for single tokens.
  * Workspace: sq_mx_linear_workspace_size bytes (0: none), 16-byte aligned.
  * Errors: as sq_mx_gemm.
  * ------------------------------------------------------------------------- */

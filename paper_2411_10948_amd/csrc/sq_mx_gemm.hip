@@ -447,6 +447,7 @@ __global__ __launch_bounds__(256) void k_mx_reduce(const float* part, int splits
 // ---------------------------------------------------------------------------
 constexpr int kRowsWaves = 8;
 
+#if defined(__HIP_DEVICE_COMPILE__)
 // 32 bf16 from an address that may be an odd multiple of two bytes: 16-byte loads
 // from such ones are split (16 x 1741 -> 1024, one launch, 7.9 us, now 5.2), so the
 // words around them are loaded and shifted.  Every word holds an element asked for.
@@ -467,6 +468,7 @@ __device__ __forceinline__ void load_halves(const uint16_t* src, uint32_t* w) {
 #pragma unroll
     for (int i = 0; i < 16; ++i) w[i] = __builtin_amdgcn_alignbit(t[i + 1], t[i], 8u * odd);
 }
+#endif
 
 // Codes and scale of 32 values in the words w (bf16 pairs, or fp32).
 template <bool BF16>
@@ -796,12 +798,14 @@ hipError_t launch_mx_gemm_pair(const MxGemmArgs& a, const MxGemmArgs& b, hipStre
 // of its own: 64 x 4096 -> 4096 in bf16 8.9 us against 13.1 with the quantizer
 // and the product, 1024 x 512 -> 512 5.5 against 6.9; 128 x 4096 -> 4096 13.5
 // against 11.7, 4096 x 512 -> 512 16.3 against 8.4, 64 x 4096 -> 4096 in fp32
-// 12.9 against 11.7.
+// 12.9 against 11.7.  Not where many blocks have a tile or less of the inner axis
+// for each of their waves: 64 experts, 512 -> 4096, 512 rows 32 against 24; 2048 ->
+// 4096, 64 rows 29 against 40.
 bool mx_rows_ok(int64_t M, int64_t K, int64_t N, int64_t experts, int type) {
-    if (M <= 16 * std::max<int64_t>(1, experts)) return true;
     const double tiles = experts ? (double)(M / 16 + std::min(experts, M)) : (double)((M + 15) / 16);
-    const double steps = (double)((K + 127) / 128) + 6.0;
-    return tiles * (double)((N + 15) / 16) * steps * (type == SQ_TYPE_F32 ? 2.0 : 1.0) <= 40000.0;
+    const double blocks = tiles * (double)((N + 15) / 16), steps = (double)((K + 127) / 128);
+    if (M <= 16 * std::max<int64_t>(1, experts)) return blocks <= 10000.0 || steps > kRowsWaves;
+    return blocks * (steps + 6.0) * (type == SQ_TYPE_F32 ? 2.0 : 1.0) <= 40000.0;
 }
 
 hipError_t launch_mx_rows(const MxRowsArgs& a, hipStream_t s) {

@@ -399,7 +399,7 @@ def test_experts_training_step(mx, name, dtype, K, N):
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
-@pytest.mark.parametrize("M,E,K,N", [(1, 4, 100, 33), (8, 64, 512, 48), (30, 3, 1000, 130), (90, 2, 96, 70),
+@pytest.mark.parametrize("M,E,K,N", [(1, 4, 100, 33), (8, 64, 512, 48), (30, 3, 1000, 130), (90, 2, 96, 70), (100, 40, 130, 4000),
                                      (1500, 5, 200, 300)])
 def test_experts_serving(mx, M, E, K, N, dtype):
     # few rows an expert (one launch) and many
