@@ -791,17 +791,20 @@ sq_status sq_mx_linear(const void* X, int32_t type, int64_t M, int64_t K, int64_
  * the caller (host struct, read during the calls only), and its three steps:
  *   sq_mx_layer_weight    codes of W [c_out, c_in] (a stack [experts] of such)
  *                         along both axes, after each update of W
- *   sq_mx_layer_forward   codes of X [rows, c_in] along both axes, Y = X W^T
+ *   sq_mx_layer_forward   codes of X [rows, c_in] along both axes, Y = X W^T; by
+ *                         expert, a copy of the offsets in `offsets`
  *   sq_mx_layer_backward  codes of dY [rows, c_out] along both axes, then
  *                         dX = dY W [rows, c_in] and dW = dY^T X [c_out, c_in]
  *                         (a stack [experts] of such, ld_dw apart in its rows)
  * Each is what sq_mx_quantize and the sq_mx_gemm calls give, in fewer launches:
  * dX and dW share one.  Y and dX have the layer's type, dW is fp32.  offsets as
- * above, NULL when experts == 0; the backward takes those of the forward, whose
- * codes of X it reads.
+ * above, NULL when experts == 0.  The backward reads codes of X that are laid out
+ * by the forward's offsets: with offsets NULL it takes the layer's copy of them,
+ * which does not change when the caller's buffer does; others must be equal.
  * Sizes: w [c_out, c_in] and w_t [c_in, c_out], each experts times; x [rows, c_in],
  * x_t [c_in, inner], dy [rows, c_out], dy_t [c_out, inner] with inner = rows, or
- * sq_mx_segment_cols(rows, experts); every one of sq_mx_size bytes.
+ * sq_mx_segment_cols(rows, experts); every one of sq_mx_size bytes.  offsets
+ * [experts + 1], or NULL: no copy is kept (nor read with experts == 0).
  * Workspace: sq_mx_layer_workspace_size bytes (0: none), 16-byte aligned.
  * Errors: as sq_mx_quantize and sq_mx_gemm.
  * ------------------------------------------------------------------------- */
@@ -814,6 +817,7 @@ typedef struct {
     uint8_t *dy, *dy_scales, *dy_t, *dy_t_scales;
     void* workspace;
     size_t workspace_bytes;
+    int32_t* offsets;                      /* the forward's, for the backward */
 } sq_mx_layer;
 
 sq_status sq_mx_layer_workspace_size(const sq_mx_layer* layer, size_t* bytes);

@@ -47,6 +47,7 @@ struct MxQuantArgs {
     uint8_t *codes, *scales;                   // blocks along the columns (may be null)
     uint8_t *codes_t, *scales_t;               // the transpose, blocks along the rows (may be null)
     int64_t cap_t;                             // inner elements of the transpose
+    int32_t* keep;                             // a copy of the offsets (may be null)
 };
 hipError_t launch_mx_quantize(const MxQuantArgs& a, hipStream_t s);
 hipError_t launch_mx_dequantize(const uint8_t* codes, const uint8_t* scales, int64_t rows, int64_t cols, void* out,

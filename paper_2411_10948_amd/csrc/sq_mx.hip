@@ -107,6 +107,8 @@ __global__ __launch_bounds__(256) void k_mx_quantize(MxQuantArgs p, uint32_t til
     const int64_t mat = blockIdx.y;
     int64_t row0 = (int64_t)tr * 128, row_end = p.rows, inner = row0;
     if (p.offsets) {
+        if (p.keep && blockIdx.x == 0)
+            for (int i = tid; i <= p.experts; i += 256) p.keep[i] = p.offsets[i];
         const Segment g = find_segment(p.offsets, p.experts, (int)p.rows, 128, (int)tr);
         if (g.expert < 0) return;
         row0 = (int64_t)g.lo + (int64_t)g.tile * 128;

@@ -137,6 +137,47 @@ MxGemmArgs dense_args(int64_t M, int64_t N, int64_t K) {
     return a;
 }
 
+// sq_mx_quantize, with a copy of the offsets in `keep` (may be NULL)
+sq_status quantize(const void* X, int32_t type, int64_t batch, int64_t rows, int64_t cols, int64_t ld, int64_t stride,
+                   const int32_t* offsets, int64_t experts, uint8_t* codes, uint8_t* scales, uint8_t* codes_t,
+                   uint8_t* scales_t, int32_t* keep, void* stream) {
+    SQ_TRY(check_type(type));
+    SQ_TRY(check_dim(batch, 65536, "batch"));
+    SQ_TRY(check_dim(rows, kMaxRows, "rows"));
+    SQ_TRY(check_dim(cols, kMaxCols, "cols"));
+    if (offsets || experts) {
+        SQ_TRY(check_experts(offsets, experts));
+        if (batch != 1) return invalid("offsets split the rows of one matrix: batch must be 1");
+    }
+    if (batch == 0 || rows == 0 || cols == 0) return SQ_OK;
+    if (!codes && !codes_t) return invalid("codes and codes_t are both NULL");
+    if (codes || scales) SQ_TRY(check_mx(codes, scales, "codes"));
+    if (codes_t || scales_t) {
+        SQ_TRY(check_mx(codes_t, scales_t, "codes_t"));
+        SQ_TRY(experts ? check_segments(rows, experts) : check_inner(rows));
+    }
+    SQ_TRY(check_values(X, type, ld, cols, "X"));
+    if (batch > 1 && (stride < 0 || stride < (rows - 1) * ld + cols)) return invalid("stride is smaller than a matrix");
+    SQ_TRY(check_blocks(rows, 128, cols, 64, experts, 2));
+    MxQuantArgs a{};
+    a.x = X;
+    a.type = type;
+    a.batch = batch;
+    a.rows = rows;
+    a.cols = cols;
+    a.ld = ld;
+    a.stride = stride;
+    a.offsets = offsets;
+    a.experts = (int)experts;
+    a.codes = codes;
+    a.scales = scales;
+    a.codes_t = codes_t;
+    a.scales_t = scales_t;
+    a.cap_t = offsets ? mx_segment_cols(rows, experts) : mx_units(rows) * kMxUnit;
+    a.keep = keep;
+    return hip_status(launch_mx_quantize(a, static_cast<hipStream_t>(stream)), "mx quantize");
+}
+
 }  // namespace
 
 extern "C" {
@@ -166,40 +207,8 @@ sq_status sq_mx_quantize(const void* X, int32_t type, int64_t batch, int64_t row
                          const int32_t* offsets, int64_t experts, uint8_t* codes, uint8_t* scales, uint8_t* codes_t,
                          uint8_t* scales_t, void* stream) {
     return guarded([&]() -> sq_status {
-        SQ_TRY(check_type(type));
-        SQ_TRY(check_dim(batch, 65536, "batch"));
-        SQ_TRY(check_dim(rows, kMaxRows, "rows"));
-        SQ_TRY(check_dim(cols, kMaxCols, "cols"));
-        if (offsets || experts) {
-            SQ_TRY(check_experts(offsets, experts));
-            if (batch != 1) return invalid("offsets split the rows of one matrix: batch must be 1");
-        }
-        if (batch == 0 || rows == 0 || cols == 0) return SQ_OK;
-        if (!codes && !codes_t) return invalid("codes and codes_t are both NULL");
-        if (codes || scales) SQ_TRY(check_mx(codes, scales, "codes"));
-        if (codes_t || scales_t) {
-            SQ_TRY(check_mx(codes_t, scales_t, "codes_t"));
-            SQ_TRY(experts ? check_segments(rows, experts) : check_inner(rows));
-        }
-        SQ_TRY(check_values(X, type, ld, cols, "X"));
-        if (batch > 1 && (stride < 0 || stride < (rows - 1) * ld + cols)) return invalid("stride is smaller than a matrix");
-        SQ_TRY(check_blocks(rows, 128, cols, 64, experts, 2));
-        MxQuantArgs a{};
-        a.x = X;
-        a.type = type;
-        a.batch = batch;
-        a.rows = rows;
-        a.cols = cols;
-        a.ld = ld;
-        a.stride = stride;
-        a.offsets = offsets;
-        a.experts = (int)experts;
-        a.codes = codes;
-        a.scales = scales;
-        a.codes_t = codes_t;
-        a.scales_t = scales_t;
-        a.cap_t = offsets ? mx_segment_cols(rows, experts) : mx_units(rows) * kMxUnit;
-        return hip_status(launch_mx_quantize(a, static_cast<hipStream_t>(stream)), "mx quantize");
+        return quantize(X, type, batch, rows, cols, ld, stride, offsets, experts, codes, scales, codes_t, scales_t, nullptr,
+                        stream);
     });
 }
 
@@ -441,6 +450,7 @@ sq_status sq_mx_layer_forward(const sq_mx_layer* layer, const void* X, int64_t l
         SQ_TRY(check_layer(layer));
         const sq_mx_layer& l = *layer;
         SQ_TRY(check_layer_offsets(layer, offsets));
+        if (l.experts && l.offsets && !aligned(l.offsets, 4)) return invalid("the layer's offsets are misaligned");
         SQ_TRY(check_product(l.rows, l.c_out, l.c_in, l.experts));
         if (l.rows > 0 && l.c_out > 0) {
             SQ_TRY(check_values(Y, l.type, ldy, l.c_out, "Y"));
@@ -450,8 +460,9 @@ sq_status sq_mx_layer_forward(const sq_mx_layer* layer, const void* X, int64_t l
             }
         }
         SQ_TRY(check_workspace(l.workspace, l.workspace_bytes, layer_workspace(layer)));
-        SQ_TRY(sq_mx_quantize(X, l.type, 1, l.rows, l.c_in, ld, 0, offsets, l.experts, l.x, l.x_scales, l.x_t, l.x_t_scales,
-                              stream));
+        // No offsets are kept where there is nothing to quantize: no result of the backward depends on them then.
+        SQ_TRY(quantize(X, l.type, 1, l.rows, l.c_in, ld, 0, offsets, l.experts, l.x, l.x_scales, l.x_t, l.x_t_scales,
+                        l.experts ? l.offsets : nullptr, stream));
         if (l.experts)
             return sq_mx_gemm_experts(l.x, l.x_scales, l.rows, l.c_in, offsets, l.experts, l.w, l.w_scales, l.c_out, Y, l.type,
                                       ldy, stream);
@@ -465,6 +476,7 @@ sq_status sq_mx_layer_backward(const sq_mx_layer* layer, const void* dY, int64_t
     return guarded([&]() -> sq_status {
         SQ_TRY(check_layer(layer));
         const sq_mx_layer& l = *layer;
+        if (!offsets && l.experts) offsets = l.offsets;
         SQ_TRY(check_layer_offsets(layer, offsets));
         SQ_TRY(check_product(l.rows, l.c_in, l.c_out, l.experts));
         SQ_TRY(check_blocks(l.c_out, 16, l.c_in, 16, 0, std::max<int64_t>(l.experts, 1)));

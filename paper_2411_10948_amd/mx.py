@@ -222,7 +222,7 @@ class Layer(ct.Structure):
     """sq_mx_layer"""
     _fields_ = ([(n, _I64) for n in ("rows", "c_in", "c_out", "experts")] + [("type", ct.c_int32), ("reserved", ct.c_int32)]
                 + [(m + s, ct.c_void_p) for m in ("w", "w_t", "x", "x_t", "dy", "dy_t") for s in ("", "_scales")]
-                + [("workspace", ct.c_void_p), ("workspace_bytes", _SZ)])
+                + [("workspace", ct.c_void_p), ("workspace_bytes", _SZ), ("offsets", ct.c_void_p)])
 
 
 def sq_mx_layer_workspace_size(layer: Layer) -> int:
@@ -262,12 +262,12 @@ def sq_mx_layer_forward(layer: Layer, X, offsets, Y, stream=None) -> None:
 
 
 def sq_mx_layer_backward(layer: Layer, dY, offsets, dX, dW, stream=None) -> None:
-    """dW [c_out, c_in] or [experts, c_out, c_in], contiguous"""
+    """dW [c_out, c_in] or [experts, c_out, c_in], contiguous; offsets None: those that the forward kept"""
     if not dW.is_contiguous():
         raise ValueError("dW: expected a contiguous tensor")
     _check("sq_mx_layer_backward", load().sq_mx_layer_backward(
         ct.addressof(layer), _of_layer(layer, dY, (layer.rows, layer.c_out), "dY"), _rows(dY, "dY"),
-        _offsets(offsets, layer.experts), _of_layer(layer, dX, (layer.rows, layer.c_in), "dX"), _rows(dX, "dX"),
+        None if offsets is None else _offsets(offsets, layer.experts), _of_layer(layer, dX, (layer.rows, layer.c_in), "dX"), _rows(dX, "dX"),
         _of_layer(layer, dW, _layer_stack(layer), "dW", TYPE_F32), max(layer.c_in, 1), _stream(stream)))
 
 
@@ -352,8 +352,8 @@ class LinearPlan:
 
     Serving: ``forward(x, w)`` with W's codes.  Training (``train=True``):
     ``quantize_weight(W)``, ``forward(x)``, then ``backward(dy)``, which gives dX in
-    the layer's type and dW in float32; the forward keeps X's codes and the
-    offsets for it.  Results are the plan's buffers, overwritten by its next
+    the layer's type and dW in float32; the forward keeps X's codes and a copy of
+    the offsets for it (``self.offsets``).  Results are the plan's buffers, overwritten by its next
     call of the same kind."""
 
     def __init__(self, M: int, C_in: int, C_out: int, dtype=torch.bfloat16, experts: int = 0, train: bool = False,
@@ -365,7 +365,7 @@ class LinearPlan:
         self._x_shape, self._y_shape = torch.Size((M, C_in)), torch.Size((M, C_out))
         self._w_shape = torch.Size((experts, C_out, C_in) if experts else (C_out, C_in))
         self.Y = torch.empty(self._y_shape, dtype=dtype, device=dev)
-        self.offsets, self._off_ptr, self._type = None, None, _TYPES[dtype]
+        self.offsets, self._type = None, _TYPES[dtype]
         self._y_ptr, self._y_ld, self._lib, self._gpu = self.Y.data_ptr(), max(C_out, 1), load(), _gpu_of(self.Y)
         self._has_weight = self._has_input = False
         if not train:
@@ -389,7 +389,10 @@ class LinearPlan:
             setattr(self.layer, name + "_scales", m.scales.data_ptr())
         self._layer_ptr, self._dw_ld = ct.addressof(self.layer), max(C_in, 1)
         self._dx_ptr, self._dw_ptr = self.dX.data_ptr(), self.dW.data_ptr()
-        self._held += [self.Y, self.dX, self.dW]
+        if experts:
+            self.offsets = torch.zeros(experts + 1, dtype=torch.int32, device=dev)
+            self.layer.offsets = self.offsets.data_ptr()
+        self._held += [self.Y, self.dX, self.dW, self.offsets]
         self.ws = _workspace(sq_mx_layer_workspace_size(self.layer), dev)
         if self.ws is not None:
             self.layer.workspace, self.layer.workspace_bytes = self.ws.data_ptr(), self.ws.nbytes
@@ -417,7 +420,7 @@ class LinearPlan:
                 self._layer_ptr, x.data_ptr(), ld, off, self._y_ptr, self._y_ld, _on(self._gpu, stream))
             if st:
                 _check("sq_mx_layer_forward", st)
-            self.offsets, self._off_ptr, self._has_input = offsets, off, True
+            self._has_input = True
             return self.Y
         if w is None or w.rows != self.C_out or w.cols != self.C_in or (w.stack or 1) != (self.experts or 1):
             raise ValueError(f"w: expected codes of {self.experts or 'one'} [{self.C_out}, {self.C_in}]")
@@ -440,7 +443,7 @@ class LinearPlan:
         if not self._has_input:
             raise ValueError("backward needs a forward before it")
         st = self._lib.sq_mx_layer_backward(
-            self._layer_ptr, dy.data_ptr(), ld, self._off_ptr, self._dx_ptr, self._dw_ld, self._dw_ptr, self._dw_ld,
+            self._layer_ptr, dy.data_ptr(), ld, None, self._dx_ptr, self._dw_ld, self._dw_ptr, self._dw_ld,
             _on(self._gpu, stream))
         if st:
             _check("sq_mx_layer_backward", st)
