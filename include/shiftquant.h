@@ -696,7 +696,9 @@ sq_status sq_l1bn_backward(const float* dy, int64_t M, int64_t C, int64_t ld_dy,
  *
  * By expert: `offsets` [experts + 1] (device memory) splits the rows; expert
  * e owns [offsets[e], offsets[e + 1]), possibly none.  Offsets ascend from
- * >= 0 to <= rows; rows outside of them are neither read nor written.
+ * >= 0 to <= rows; rows outside of them are neither read nor written (of codes,
+ * padded to whole groups of 16 rows, products read the groups that experts' rows
+ * are in).
  * Offsets that break this never lead out of the buffers, but what is
  * computed is then unspecified.  The inner axis of the transposed form
  * starts anew at a multiple of 512 for each expert: expert e's rows are

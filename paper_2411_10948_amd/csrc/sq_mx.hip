@@ -105,15 +105,21 @@ __global__ __launch_bounds__(256) void k_mx_quantize(MxQuantArgs p, uint32_t til
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const uint32_t tr = blockIdx.x / tiles_c, tc = blockIdx.x - tr * tiles_c;
     const int64_t mat = blockIdx.y;
-    int64_t row0 = (int64_t)tr * 128, row_end = p.rows, inner = row0;
+    int64_t row0 = (int64_t)tr * 128, row_first = row0, row_end = p.rows, inner = row0;
     if (p.offsets) {
         if (p.keep && blockIdx.x == 0)
             for (int i = tid; i <= p.experts; i += 256) p.keep[i] = p.offsets[i];
-        const Segment g = find_segment(p.offsets, p.experts, (int)p.rows, 128, (int)tr);
-        if (g.expert < 0) return;
-        row0 = (int64_t)g.lo + (int64_t)g.tile * 128;
-        row_end = g.hi;
-        inner = g.inner + (int64_t)g.tile * 128;
+        if (p.codes_t) {
+            const Segment g = find_segment(p.offsets, p.experts, (int)p.rows, 128, (int)tr);
+            if (g.expert < 0) return;
+            row0 = row_first = (int64_t)g.lo + (int64_t)g.tile * 128;
+            row_end = g.hi;
+            inner = g.inner + (int64_t)g.tile * 128;
+        } else {    // blocks along the columns alone: no tile has to start at an expert's first row, rows of none stay out
+            row_first = min(max((int64_t)p.offsets[0], (int64_t)0), p.rows);
+            row_end = min(max((int64_t)p.offsets[p.experts], row_first), p.rows);
+            if (row0 + 128 <= row_first || row0 >= row_end) return;
+        }
     }
     const int64_t col0 = (int64_t)tc * TC;
     const T* x = static_cast<const T*>(p.x) + mat * p.stride;
@@ -128,7 +134,7 @@ __global__ __launch_bounds__(256) void k_mx_quantize(MxQuantArgs p, uint32_t til
         const T* src = x + r * p.ld + c;
 #pragma unroll
         for (int w = 0; w < kWords; ++w) v[i][w] = 0;
-        if (r >= row_end || left <= 0) continue;
+        if (r < row_first || r >= row_end || left <= 0) continue;
         if (left >= 8) {
 #pragma unroll
             for (int w = 0; w < kWords; w += 4) {
@@ -197,7 +203,7 @@ __global__ __launch_bounds__(256) void k_mx_quantize(MxQuantArgs p, uint32_t til
             const int j = lane & 3;
             const int64_t r = row0 + r0 + (i + j) * kPass, group = (r >> 4) * units;
             const int slot = (int)(r & 15);
-            if (r < row_end) {
+            if (r >= row_first && r < row_end) {
                 *reinterpret_cast<uint4*>(codes + group * kMxUnitBytes + slot * 16) = make_uint4(k[0], k[1], k[2], k[3]);
                 scales[group * kMxUnitScales + slot * 4] = (uint8_t)(j & 2 ? (j & 1 ? s[3] : s[2]) : (j & 1 ? s[1] : s[0]));
             }
@@ -274,7 +280,7 @@ hipError_t quantize(const MxQuantArgs& a, hipStream_t s) {
     constexpr int TC = QuantTile<T>::TC;
     // whole 128-element tiles of the columns, so that the row codes' padding is written too
     const int64_t tiles_c = round_up(a.cols, kMxTile) / TC;
-    const int64_t tiles_r = a.offsets ? a.rows / 128 + std::min<int64_t>(a.experts, a.rows) : (a.rows + 127) / 128;
+    const int64_t tiles_r = a.offsets && a.codes_t ? a.rows / 128 + std::min<int64_t>(a.experts, a.rows) : (a.rows + 127) / 128;
     // Inputs that the last-level cache would not keep anyway are read past it, so
     // that the codes stay there for the product: 8192 x 4096 in bf16 and its product
     // with 11008 columns 208 -> 195 us; a step of 3152 x 768 x 768 in fp32 29.0 ->

@@ -383,7 +383,7 @@ sq_status sq_mx_linear(const void* X, int32_t type, int64_t M, int64_t K, int64_
         }
         uint8_t* codes = static_cast<uint8_t*>(workspace);
         uint8_t* scales = codes + w.codes;
-        SQ_TRY(sq_mx_quantize(X, type, 1, M, K, ld, 0, nullptr, 0, codes, scales, nullptr, nullptr, stream));
+        SQ_TRY(sq_mx_quantize(X, type, 1, M, K, ld, 0, offsets, experts, codes, scales, nullptr, nullptr, stream));
         if (experts)
             return sq_mx_gemm_experts(codes, scales, M, K, offsets, experts, W, W_scales, N, Y, out_type, ldy, stream);
         return sq_mx_gemm(codes, scales, W, W_scales, M, N, K, Y, out_type, ldy, scales + w.scales, w.part, stream);

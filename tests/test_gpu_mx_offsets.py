@@ -67,3 +67,63 @@ def test_two_layers_share_one_buffer_of_offsets(mx):
         shared.append(plan.backward(dy))
     for a, b in zip(alone, shared):
         assert torch.equal(a[0], b[0]) and torch.equal(a[1], b[1])
+
+
+OUTSIDE = [(2000, 520, 700, [300, 300, 900, 1500]), (4100, 300, 600, [0, 5, 4000]), (2100, 1030, 800, [2050, 2051, 2100]),
+           (3000, 256, 1100, [7] * 9)]
+
+
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
+@pytest.mark.parametrize("M,K,N,off", OUTSIDE)
+def test_rows_outside_are_left_alone(mx, M, K, N, off, dtype):
+    # the serving call that quantizes first: its codes of rows that no expert has, and their outputs, keep what they held
+    import torch
+    dt, E = getattr(torch, dtype), len(off) - 1
+    g = torch.Generator(device="cuda").manual_seed(M)
+    x = torch.randn(M, K, generator=g, device="cuda").to(dt)
+    w = torch.randn(E, N, K, generator=g, device="cuda").to(dt)
+    plan = mx.LinearPlan(M, K, N, dtype=dt, experts=E)
+    assert plan.ws is not None      # not the call of few rows, which has no codes
+    plan.ws.fill_(0x5A)
+    plan.Y.fill_(7.0)
+    y = plan.forward(x, mx.quantize(w)[0], _ints(off)).double().cpu().numpy()
+    byte, _, sc = ref.mx_places(M, K)
+    ws, at = plan.ws.cpu().numpy(), -(-mx.sq_mx_size(M, K)[0] // 256) * 256
+    out = np.ones(M, bool)
+    out[off[0]:off[-1]] = False
+    assert (ws[byte][out] == 0x5A).all() and (ws[at:][sc][out] == 0x5A).all() and (y[out] == 7.0).all()
+    xv, wv = x.double().cpu().numpy(), w.double().cpu().numpy()
+    codes, scales = ref.mx_unpack(ws, ws[at:], M, K)
+    k, s = ref.mx_codes(xv)
+    np.testing.assert_array_equal(codes[~out], k.reshape(M, -1)[~out, :K])
+    np.testing.assert_array_equal(scales[~out], np.repeat(s, 32, -1)[~out, :K])
+    for e, (lo, hi) in enumerate(ref.segments(off)):
+        if hi == lo:
+            continue
+        want, mag = ref.mx_product(ref.mx_values(xv[lo:hi]), ref.mx_values(wv[e]))
+        tol = mag * (K + 2) * 2.0 ** -23        # an fp32 sum of K exact products, then one rounding
+        if dtype == "bfloat16":
+            tol = tol + (np.abs(want) + tol) * 2.0 ** -8
+        assert (np.abs(y[lo:hi] - want) <= tol).all()
+
+
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
+@pytest.mark.parametrize("off", [[0, 64, 256], [5, 37, 37, 200], [0] * 70 + [3] * 30 + [250], [17, 17], [130, 131], [256, 256]])
+def test_quantize_rows_by_expert(mx, off, dtype):
+    # codes along the columns alone, with offsets: inside as ever, outside untouched
+    import torch
+    M, C, E = 256, 200, len(off) - 1
+    x = torch.randn(M, C, generator=torch.Generator(device="cuda").manual_seed(E), device="cuda").to(getattr(torch, dtype))
+    a = mx.MxMatrix.empty(M, C)
+    a.codes.fill_(0x5A)
+    a.scales.fill_(0x5A)
+    mx.sq_mx_quantize(x, a.codes, a.scales, None, None, _ints(off), E)
+    byte, _, sc = ref.mx_places(M, C)
+    codes, scales = a.codes.view(-1).cpu().numpy(), a.scales.view(-1).cpu().numpy()
+    out = np.ones(M, bool)
+    out[off[0]:off[-1]] = False
+    assert (codes[byte][out] == 0x5A).all() and (scales[sc][out] == 0x5A).all()
+    got, s8 = ref.mx_unpack(codes, scales, M, C)
+    k, s = ref.mx_codes(x.double().cpu().numpy())
+    np.testing.assert_array_equal(got[~out], k.reshape(M, -1)[~out, :C])
+    np.testing.assert_array_equal(s8[~out], np.repeat(s, 32, -1)[~out, :C])
