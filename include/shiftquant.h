@@ -694,6 +694,10 @@ sq_status sq_l1bn_backward(const float* dy, int64_t M, int64_t C, int64_t ld_dy,
  * and never used.  Matrices of a stack follow each other without a gap.
  * codes must be 16-byte aligned, scales 4-byte.
  *
+ * Sizes, SQ_ERR_INVALID_ARGUMENT otherwise: rows < 2^31; columns of values (cols,
+ * N, c_in, c_out, K of sq_mx_linear) < 2^20; experts < 2^16; batch < 2^16.  Inner
+ * axes of products: see each call.
+ *
  * By expert: `offsets` [experts + 1] (device memory) splits the rows; expert
  * e owns [offsets[e], offsets[e + 1]), possibly none.  Offsets ascend from
  * >= 0 to <= rows; rows outside of them are neither read nor written (of codes,

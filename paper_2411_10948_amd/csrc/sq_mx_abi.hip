@@ -128,6 +128,12 @@ sq_status check_product(int64_t M, int64_t N, int64_t K, int64_t experts) {
     return check_blocks(M, 16, N, 16, experts, 1);
 }
 
+// of a product whose A is quantized on the way: K is the columns of its values too
+sq_status check_linear(int64_t M, int64_t N, int64_t K, int64_t experts) {
+    SQ_TRY(check_product(M, N, K, experts));
+    return M == 0 || N == 0 ? SQ_OK : check_dim(K, kMaxCols, "K");
+}
+
 MxGemmArgs dense_args(int64_t M, int64_t N, int64_t K) {
     MxGemmArgs a{};
     a.mode = kDense;
@@ -338,7 +344,7 @@ sq_status sq_mx_gemm_experts_wgrad(const uint8_t* A, const uint8_t* A_scales, co
 sq_status sq_mx_linear_workspace_size(int64_t M, int64_t K, int64_t N, int64_t experts, size_t* bytes) {
     return guarded([&]() -> sq_status {
         if (experts < 0 || experts >= kMaxExperts) return invalid("experts is out of range");
-        SQ_TRY(check_product(M, N, K, experts));
+        SQ_TRY(check_linear(M, N, K, experts));
         if (!bytes) return invalid("bytes is NULL");
         *bytes = std::max(linear_workspace(M, K, N, experts, SQ_TYPE_F32).bytes(),
                           linear_workspace(M, K, N, experts, SQ_TYPE_BF16).bytes());
@@ -353,9 +359,8 @@ sq_status sq_mx_linear(const void* X, int32_t type, int64_t M, int64_t K, int64_
         SQ_TRY(check_type(type));
         SQ_TRY(check_type(out_type));
         if (offsets || experts) SQ_TRY(check_experts(offsets, experts));
-        SQ_TRY(check_product(M, N, K, experts));
+        SQ_TRY(check_linear(M, N, K, experts));
         if (M == 0 || N == 0) return SQ_OK;
-        SQ_TRY(check_dim(K, kMaxCols, "K"));
         if (K > 0) {
             SQ_TRY(check_values(X, type, ld, K, "X"));
             SQ_TRY(check_mx(W, W_scales, "W"));

@@ -39,3 +39,24 @@ def test_offsets_of_the_backward(mx):
     assert forward == INVALID and "offsets" in sq_last_error()
     # the forward does not take the copy for the caller's
     assert L.sq_mx_layer_forward(_layer(mx), P, 64, None, P, 64, None) == INVALID
+
+
+def test_the_size_of_a_workspace_is_refused_where_the_call_is(mx):
+    from paper_2411_10948_amd.shiftquant import load
+    L, n = load(), ct.c_size_t(0)
+    most = 1 << 20
+
+    def size(M, K, N, e=0):
+        return L.sq_mx_linear_workspace_size(M, K, N, e, ct.byref(n))
+
+    def linear(M, K, N, off=None, e=0):
+        # no workspace: what is not refused for its sizes is for that
+        return L.sq_mx_linear(P, 0, M, K, K, off, e, P, P, N, P, 0, N, None, 0, None)
+
+    for M, K, N in [(4096, most, 64), (4096, (1 << 23) - 1, 64), (1, most, 64), (4096, 64, most), (1 << 31, 64, 64)]:
+        assert size(M, K, N) == INVALID and linear(M, K, N) == INVALID
+    assert size(4096, 1 << 23, 64) == linear(4096, 1 << 23, 64) == UNSUPPORTED
+    assert size(4096, 64, 64, 1 << 16) == linear(4096, 64, 64, P, 1 << 16) == INVALID
+    assert size(4096, most - 1, 64) == 0 and n.value > 0
+    for M, N in ((0, 64), (64, 0)):     # nothing to compute
+        assert size(M, most, N) == 0 and n.value == 0 and linear(M, most, N) == 0
