@@ -71,10 +71,13 @@ __device__ __forceinline__ void store8(T* row, int64_t c, int64_t cols, const fl
 
 constexpr float kGeluA = 1.5957691216057308f, kGeluB = 0.044715f;   // 2 sqrt(2 / pi)
 
-// sigma(t), and t' for the slope.  sigma is 1 or t's exponential to fp32 well
-// before |x| = 60, so GELU's cube is taken there, where nothing overflows.
-template <int KIND>
-__device__ __forceinline__ float gate(float x, float& slope) {
+// sigma(t), 1 - sigma(t), and t' for the slope.  sigma is 1 or t's exponential to
+// fp32 well before |x| = 60, so GELU's cube is taken there, where nothing overflows.
+// fp32: e = exp(-|t|) to 1 ulp and sigma = e / (1 + e) or 1 / (1 + e), so that
+// neither end loses digits; with __expf, which rounds the argument's product with
+// log2 e, SiLU at -80 is off by 4e-6 of its value.  bf16 rounds both to the same.
+template <int KIND, bool F32>
+__device__ __forceinline__ float gate(float x, float& rest, float& slope) {
     float t = x;
     slope = 1.0f;
     if constexpr (KIND == SQ_ACT_GELU) {
@@ -82,7 +85,15 @@ __device__ __forceinline__ float gate(float x, float& slope) {
         t = kGeluA * (y + kGeluB * y2 * y);
         slope = kGeluA * (1.0f + 3.0f * kGeluB * y2);
     }
-    return __builtin_amdgcn_rcpf(1.0f + __expf(-t));
+    if constexpr (F32) {
+        const float e = expf(-fabsf(t)), r = __builtin_amdgcn_rcpf(1.0f + e), er = e * r;
+        rest = t < 0.0f ? r : er;
+        return t < 0.0f ? er : r;
+    } else {
+        const float sg = __builtin_amdgcn_rcpf(1.0f + __expf(-t));
+        rest = 1.0f - sg;
+        return sg;
+    }
 }
 
 // The 8-bit copy of 8 elements; four lanes hold a block of 32.
@@ -160,8 +171,8 @@ __global__ __launch_bounds__(256) void k_act_forward(ActArgs p, ActGrid q) {
     }
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
-        float slope;
-        h[e] = g[e] * gate<KIND>(g[e], slope);
+        float rest, slope;
+        h[e] = g[e] * gate<KIND, sizeof(T) == 4>(g[e], rest, slope);
         if constexpr (GATED) h[e] *= u[e];
     }
     store8<T>(static_cast<T*>(p.h) + r * p.ld_h, c, p.F, h);
@@ -184,9 +195,9 @@ __global__ __launch_bounds__(256) void k_act_backward(ActArgs p, ActGrid q) {
     values8<T>(dw, d);
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
-        float slope;
-        const float sg = gate<KIND>(g[e], slope), a = g[e] * sg;
-        const float da = sg + a * (1.0f - sg) * slope;
+        float rest, slope;
+        const float sg = gate<KIND, sizeof(T) == 4>(g[e], rest, slope), a = g[e] * sg;
+        const float da = sg + a * rest * slope;
         if constexpr (GATED) {
             g[e] = d[e] * u[e] * da;
             u[e] = d[e] * a;
