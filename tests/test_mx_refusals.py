@@ -60,3 +60,32 @@ def test_the_size_of_a_workspace_is_refused_where_the_call_is(mx):
     assert size(4096, most - 1, 64) == 0 and n.value > 0
     for M, N in ((0, 64), (64, 0)):     # nothing to compute
         assert size(M, most, N) == 0 and n.value == 0 and linear(M, most, N) == 0
+
+
+def test_the_workspace_of_split_sums(mx):
+    # few tiles of a long inner axis: the partial sums are the caller's, and never written where there are none
+    from paper_2411_10948_amd.shiftquant import load, sq_last_error
+    L, n = load(), ct.c_size_t(0)
+    odd = ct.c_void_p(0x100008)
+    M, N, K = 64, 640, 30000
+    assert L.sq_mx_gemm_workspace_size(M, N, K, ct.byref(n)) == 0 and n.value >= 2 * M * N * 4
+
+    def gemm(ws, nws):
+        return L.sq_mx_gemm(P, P, P, P, M, N, K, P, 0, N, ws, nws, None)
+
+    assert gemm(None, n.value) == INVALID and "workspace" in sq_last_error()
+    assert gemm(odd, n.value) == INVALID
+    assert gemm(P, n.value - 1) == SMALL and gemm(P, 0) == SMALL
+    part = n.value
+
+    M, N, K = 128, 1024, 12288          # the same behind a quantizer: codes, scales and partial sums
+    assert L.sq_mx_gemm_workspace_size(M, N, K, ct.byref(n)) == 0 and n.value >= 2 * M * N * 4
+    part = n.value
+    assert L.sq_mx_linear_workspace_size(M, K, N, 0, ct.byref(n)) == 0
+    assert n.value >= sum(mx.sq_mx_size(M, K)) + part
+
+    def linear(ws, nws):
+        return L.sq_mx_linear(P, 0, M, K, K, None, 0, P, P, N, P, 0, N, ws, nws, None)
+
+    assert linear(None, n.value) == INVALID and linear(odd, n.value) == INVALID and linear(P, n.value - 1) == SMALL
+    assert linear(P, n.value - part) == SMALL
