@@ -4,9 +4,9 @@ copy, then serve single tokens from its 4-bit weights.
     python examples/expert_mlp.py [--steps 60] [--tokens 512] [--dim 256] [--hidden 384] [--experts 8] [--top-k 2]
 
 The target is a fixed random layer of the same shape computed in fp32; the data
-are synthetic and seeded.  Prints the loss as it falls, the bytes that the
-backward pass is kept for, and how far the served tokens are from the trained
-layer's own forward.
+are synthetic and seeded.  Prints the loss as it falls, the bytes of the codes
+that the backward pass reads in place of tensors and of all the layer's buffers,
+and how far the served tokens are from the trained layer's own forward.
 """
 import argparse
 import os
@@ -36,7 +36,9 @@ def run(steps=60, tokens=512, dim=256, hidden=384, experts=8, top_k=2, lr=2e-3, 
     weights = {k: v + 0.3 * rand(*v.shape) / v.shape[-1] ** 0.5 for k, v in goal.items()}
     moments = {k: (torch.zeros_like(v), torch.zeros_like(v)) for k, v in weights.items()}
 
+    held = torch.cuda.memory_allocated()
     layer = ExpertMLP(tokens, dim, hidden, experts, top_k)
+    held = torch.cuda.memory_allocated() - held
     first = last = None
     for step in range(1, steps + 1):
         x = rand(tokens, dim)
@@ -54,8 +56,9 @@ def run(steps=60, tokens=512, dim=256, hidden=384, experts=8, top_k=2, lr=2e-3, 
             log(f"step {step:3d}  loss {last:.5f}", flush=True)
     kept = sum(t.numel() for t in (layer.up.x_t.codes, layer.up.x_t.scales, layer.down.x_t.codes, layer.down.x_t.scales,
                                    layer.act.codes, layer.act.scales))
-    log(f"kept for the backward pass: {kept / 1e6:.2f} MB; in bf16 the same tensors are "
-        f"{2 * tokens * top_k * (dim + 3 * hidden) / 1e6:.2f} MB (segments of 512 rows an expert included in the former)")
+    log(f"codes that the backward pass reads: {kept / 1e6:.2f} MB (segments of 512 rows an expert included); the same "
+        f"tensors in bf16: {2 * tokens * top_k * (dim + 3 * hidden) / 1e6:.2f} MB; all of the layer's buffers, weights' codes, "
+        f"outputs and gradients among them: {held / 1e6:.2f} MB")
 
     one = ExpertMLP(1, dim, hidden, experts, top_k, train=False)
     w = weights["w1"].bfloat16(), weights["w2"].bfloat16()

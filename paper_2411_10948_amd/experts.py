@@ -4,9 +4,12 @@ and its outputs are added up by the router's weights.
 
 Forward and backward use, in order: the products by expert (``LinearPlan`` with
 ``experts``), the gated activation with its 8-bit copy (``ActPlan``) and the
-products by expert again.  Between the two passes the layer keeps the 4-bit codes
-of both products' inputs and 33/32 bytes an element of the activation's input.
-Routing (softmax, top-k, a stable sort) is torch's.
+products by expert again.  The backward pass reads the 4-bit codes of both
+products' inputs, 33/32 bytes an element of the activation's input, and, for the
+router's gradient, x and the chosen experts' outputs [tokens, top_k, dim].  What is
+allocated is more: the plans hold their outputs and gradients in full as long as
+the layer lives.  In serving the activation writes its copy too, which nothing
+reads then.  Routing (softmax, top-k, a stable sort) is torch's.
 """
 from __future__ import annotations
 
