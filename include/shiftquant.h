@@ -767,7 +767,8 @@ sq_status sq_mx_gemm_experts(const uint8_t* A, const uint8_t* A_scales, int64_t 
  * A[:, r] B[:, r]^T: A [M, sq_mx_segment_cols(rows, experts)] and B [N, same]
  * are the transposed forms that sq_mx_quantize wrote with the same offsets;
  * C is a stack [experts] of [M, ldc].  An expert without rows gets zeros.
- * Workspace: sq_mx_gemm_experts_wgrad_workspace_size bytes (0: none).
+ * Workspace: sq_mx_gemm_experts_wgrad_workspace_size bytes (0: none; no size needs
+ * one, the inner axis is not split).
  * Errors: as sq_mx_gemm; SQ_ERR_UNSUPPORTED for rows >= 2^23.
  * ------------------------------------------------------------------------- */
 sq_status sq_mx_gemm_experts_wgrad_workspace_size(int64_t rows, int64_t experts, int64_t M, int64_t N, size_t* bytes);

@@ -7,9 +7,10 @@
 // scale byte for 32 consecutive elements of g or of u (mx_scale8).  A training
 // step keeps 33/32 bytes per input element instead of 2 or 4.  One pass over the
 // data, eight elements a thread, bound by HBM: gated SiLU of 8192 x 11008 in bf16
-// 125 us forward and 119 backward (727 MB each, 5.8 and 6.1 TB/s; 132 and 130
-// with ordinary instead of nontemporal stores and twice the vector
-// instructions: a 64-bit division a thread, maxima and codes element by element).
+// (727 MB a direction), each repeated, 125 us forward and 119 backward (5.8 and 6.1
+// TB/s); in turn, as in a training step, 114 and 135, together 249.  With ordinary
+// instead of nontemporal stores and twice the vector instructions (a 64-bit
+// division a thread, maxima and codes element by element) 132 and 130.
 #include <algorithm>
 
 #include "sq_mx.h"

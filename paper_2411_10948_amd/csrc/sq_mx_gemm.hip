@@ -12,11 +12,12 @@
 // What bounds the large products is power: the register-only loop of the
 // instruction runs at 9.8 PFLOP/s on zeros and at 7.1 on random codes and scales,
 // 7.2 with one operand of each instruction that of the one before, as the shader
-// clock falls.  The whole kernel
-// reaches 4.8 at 8192 x 4096 x 44032 (5.8 on zeros), 4.1 to 4.5 at 8192 x 4096 x
-// 11008 (164 to 180 us) and 3.7 at 8192 x 11008 x 4096 (197 us, a bf16 library
-// product of the same size 3.2 times as long); without the loop's loads from
-// the L2 it would be at the power limit, without their waits no faster.
+// clock falls; and the same launch of this kernel is 20 to 28 % shorter on zeros.
+// Back to back, on quantized normal values and on zeros: 8192 x 4096 x 44032 609
+// and 500 us (4.85 and 5.9 PFLOP/s), 8192 x 4096 x 11008 172 and 124 (4.3 and 5.9),
+// 8192 x 11008 x 4096 191 and 141 (3.9 and 5.2; a bf16 library product of this size
+// takes 3.2 times as long).  With the clock that a launch happens to get the
+// normal values' times spread by 167 to 197 and 183 to 216 us.
 #include <algorithm>
 #include <type_traits>
 
@@ -729,8 +730,10 @@ hipError_t rows(const MxRowsArgs& a, int64_t tiles_m, hipStream_t s) {
 
 // 64 columns a block where blocks of 16 would be more than two a CU (one row,
 // 4096 -> 11008, 688 of them: 7.5 us against 8.3; 64 experts, 64 rows, 2048 ->
-// 1024: 12.4 against 16.3; one row, 4096 -> 4096, 256: 5.6 against 4.7).  fp32
-// values fill the registers with one tile in flight.
+// 1024: 12.4 against 16.3; one row, 4096 -> 4096, 256: 5.6 against 4.7).
+// bf16 has two tiles in flight, fp32 one: 16 rows, 11008 -> 4096, 22.5 us and 24.2
+// with two; 8200 -> 8197 21.4 and 24.2; one row, 4096 -> 4096, 4.5 and 4.6; 64 rows on
+// 64 experts, 2048 -> 1024, 16.0 and 15.0.
 template <typename T>
 hipError_t rows_of(const MxRowsArgs& a, hipStream_t s) {
     const int64_t tiles_m = a.offsets ? a.M / 16 + std::min<int64_t>(a.experts, a.M) : (a.M + 15) / 16;
