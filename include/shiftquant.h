@@ -862,6 +862,106 @@ sq_status sq_act_forward(const void* X, int32_t type, int32_t kind, int32_t gate
 sq_status sq_act_backward(const void* dH, int32_t type, int32_t kind, int32_t gated, int64_t M, int64_t F, int64_t ld_h,
                           const int8_t* codes, const uint8_t* scales, void* dX, int64_t ld_x, void* stream);
 
+/* =========================================================================
+ * What stands around an expert layer's products: layer norm, the router, and the
+ * exchange of rows between tokens and experts.  Rows are fp32 or bf16
+ * (SQ_TYPE_*) with a row stride; sums, statistics and scores are fp32 or fp64,
+ * results are rounded once to their type.  Results do not depend on how the work
+ * is split over the GPU in another run: no sum is added up by atomics.
+ * ========================================================================= */
+
+/* ---------------------------------------------------------------------------
+ * sq_norm_forward, sq_norm_backward -- layer norm of the rows of X [M, C], with the
+ * residual sum before it.
+ *   h = x, or x + residual rounded to the type (H [M, C]; both NULL or neither)
+ *   mean, var of a row of h (var: divided by C);  r = 1 / sqrt(var + eps)
+ *   y = (h - mean) r gamma + beta
+ *   q = dy gamma, xh = (h - mean) r:
+ *   dx = r (q - mean(q) - xh mean(q xh)) (+ dh);  dgamma = sum_rows dy xh;  dbeta = sum_rows dy
+ * gamma and beta [C] of param_type, dgamma and dbeta [C] fp32.  The backward reads
+ * h (X without a residual) and the forward's stats [M, 4] (fp32, 16-byte aligned;
+ * the forward takes NULL where there is no backward); dH, the gradient that
+ * reaches h past the norm, may be NULL; dX is the gradient of x and of the
+ * residual.  M = 0 gives dgamma = dbeta = 0.  A row that holds NaN or Inf gives
+ * NaN in all of its y and dx, and in all of dgamma.  H may be X or residual, dX
+ * may be dH, in place; no other buffers overlap.  M < 2^31, C < 2^20.
+ * Workspace: sq_norm_backward_workspace_size bytes, 16-byte aligned.
+ * Errors: SQ_ERR_INVALID_ARGUMENT, SQ_ERR_WORKSPACE_TOO_SMALL, SQ_ERR_HIP.
+ * ------------------------------------------------------------------------- */
+sq_status sq_norm_forward(const void* X, const void* residual, int32_t type, int64_t M, int64_t C, int64_t ld_x, int64_t ld_r,
+                          const void* gamma, const void* beta, int32_t param_type, float eps,
+                          void* H, int64_t ld_h, void* Y, int64_t ld_y, float* stats, void* stream);
+sq_status sq_norm_backward_workspace_size(int64_t M, int64_t C, size_t* bytes);
+sq_status sq_norm_backward(const void* dY, const void* H, const void* dH, int32_t type, int64_t M, int64_t C,
+                           int64_t ld_dy, int64_t ld_h, int64_t ld_dh, const void* gamma, int32_t param_type, const float* stats,
+                           void* dX, int64_t ld_dx, float* dgamma, float* dbeta,
+                           void* workspace, size_t workspace_bytes, void* stream);
+
+/* ---------------------------------------------------------------------------
+ * sq_route_forward -- the k best of E experts for each of T tokens, by their logits
+ * [T, E], and where each token's rows go.
+ *   SQ_SCORE_SOFTMAX  s = softmax(logits)       SQ_SCORE_SIGMOID  s_e = 1 / (1 + exp(-logit_e))
+ * Experts are ordered by their logits, with a bias [E] (fp32, may be NULL) by
+ * s + bias: the bias moves the choice, not the shares.  An expert whose logit (or
+ * s + bias) is -Inf is never chosen.  groups > 1: the experts are `groups` runs of
+ * E / groups; a group counts as the sum of its two highest s (+ bias), and experts
+ * outside of the top_groups best groups are left out.  Equal ones: the lowest
+ * index.  Comparisons of s are made in fp64.
+ *   chosen [T, k]  the experts, best first; -1 where there are no more
+ *   share  [T, k]  scale s_e, renormalize: scale s_e / sum of the chosen s (at least
+ *                  1e-300); fp32; 0 where chosen is -1
+ *   place  [T, k]  the position of (token, slot) in a stable sort of all of them by
+ *                  expert: token t's row of expert e; -1 where chosen is -1
+ *   offsets [E + 1] rows of expert e: [offsets[e], offsets[e + 1])
+ * A token with NaN among its logits (or s + bias), or +Inf under softmax, has
+ * chosen = place = -1 and share NaN.
+ * Sizes: T < 2^26, T k < 2^31, E <= 1024, k <= 64, groups <= 64 (SQ_ERR_UNSUPPORTED).
+ * Workspace: sq_route_workspace_size bytes (0: none), 16-byte aligned.
+ *
+ * sq_route_backward -- the logits' gradient from dshare [T, k], the forward's
+ * logits, share and chosen (the choice has no gradient); slots with chosen = -1
+ * count for nothing, a token whose shares are NaN gets NaN.  Every element of
+ * dlogits [T, E] is written; it may be the logits, in place.
+ * Errors: SQ_ERR_INVALID_ARGUMENT, SQ_ERR_UNSUPPORTED, SQ_ERR_WORKSPACE_TOO_SMALL,
+ * SQ_ERR_HIP.
+ * ------------------------------------------------------------------------- */
+enum {
+    SQ_SCORE_SOFTMAX = 0,
+    SQ_SCORE_SIGMOID = 1
+};
+
+sq_status sq_route_workspace_size(int64_t T, int64_t E, size_t* bytes);
+sq_status sq_route_forward(const void* logits, int32_t type, int64_t T, int64_t E, int64_t ld, const float* bias,
+                           int32_t score, int32_t k, int32_t groups, int32_t top_groups, int32_t renormalize, float scale,
+                           float* share, int32_t* chosen, int32_t* place, int32_t* offsets,
+                           void* workspace, size_t workspace_bytes, void* stream);
+sq_status sq_route_backward(const float* dshare, const void* logits, int32_t type, int64_t T, int64_t E, int64_t ld,
+                            int32_t score, int32_t k, int32_t renormalize, float scale,
+                            const float* share, const int32_t* chosen, void* dlogits, int64_t ld_d, void* stream);
+
+/* ---------------------------------------------------------------------------
+ * sq_exchange_* -- rows [T, D] of tokens to rows [rows, D] sorted by expert and
+ * back; place [T, k] and share [T, k] (fp32) as sq_route_forward writes them.
+ *   dispatch          R[place[t, j]] = X[t]
+ *   combine           out[t] = add[t] + sum_j share[t, j] R[place[t, j]]
+ *                     (add NULL: 0; share NULL: 1, which is dispatch's gradient)
+ *   combine_backward  dR[place[t, j]] = share[t, j] dout[t],
+ *                     dshare[t, j] = sum_d dout[t, d] R[place[t, j], d]
+ * A place outside [0, rows) is no row: it is neither read nor written, adds
+ * nothing (whatever its share), and its dshare is 0.  No place comes twice.  Rows
+ * that no place names stay as they were.  `add` may be out, in place; no other
+ * buffers overlap.  T k < 2^31, k <= 64 (SQ_ERR_UNSUPPORTED), D < 2^20.
+ * Errors: SQ_ERR_INVALID_ARGUMENT, SQ_ERR_UNSUPPORTED, SQ_ERR_HIP.
+ * ------------------------------------------------------------------------- */
+sq_status sq_exchange_dispatch(const void* X, int32_t type, int64_t T, int64_t D, int64_t ld_x, const int32_t* place, int32_t k,
+                               void* R, int64_t rows, int64_t ld_r, void* stream);
+sq_status sq_exchange_combine(const void* R, int32_t type, int64_t rows, int64_t D, int64_t ld_r,
+                              const int32_t* place, const float* share, int64_t T, int32_t k,
+                              const void* add, int64_t ld_add, void* out, int64_t ld_out, void* stream);
+sq_status sq_exchange_combine_backward(const void* dout, const void* R, int32_t type, int64_t rows, int64_t D,
+                                       int64_t ld_dout, int64_t ld_r, const int32_t* place, const float* share, int64_t T, int32_t k,
+                                       void* dR, int64_t ld_dr, float* dshare, void* stream);
+
 /* Static description of a status code. */
 const char* sq_status_string(sq_status s);
 

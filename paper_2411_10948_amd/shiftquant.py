@@ -52,6 +52,8 @@ EXPORTS = (
     "sq_mx_gemm_experts", "sq_mx_gemm_experts_wgrad_workspace_size", "sq_mx_gemm_experts_wgrad",
     "sq_mx_linear_workspace_size", "sq_mx_linear", "sq_mx_layer_workspace_size", "sq_mx_layer_weight",
     "sq_mx_layer_forward", "sq_mx_layer_backward", "sq_act_size", "sq_act_forward", "sq_act_backward",
+    "sq_norm_forward", "sq_norm_backward_workspace_size", "sq_norm_backward", "sq_route_workspace_size", "sq_route_forward",
+    "sq_route_backward", "sq_exchange_dispatch", "sq_exchange_combine", "sq_exchange_combine_backward",
     "sq_status_string", "sq_last_error", "sq_last_error_string",
 )
 
@@ -189,6 +191,18 @@ def load() -> ct.CDLL:
         "sq_act_size": [_I64, _I64, i32, ct.POINTER(_SZ), ct.POINTER(_SZ)],
         "sq_act_forward": [_P, i32, i32, i32, _I64, _I64, _I64, _P, _I64, _P, _P, _P],
         "sq_act_backward": [_P, i32, i32, i32, _I64, _I64, _I64, _P, _P, _P, _I64, _P],
+    })
+    f32 = ct.c_float
+    sig.update({   # wrapped in the norm and route modules
+        "sq_norm_forward": [_P, _P, i32, _I64, _I64, _I64, _I64, _P, _P, i32, f32, _P, _I64, _P, _I64, _P, _P],
+        "sq_norm_backward_workspace_size": [_I64, _I64, ct.POINTER(_SZ)],
+        "sq_norm_backward": [_P, _P, _P, i32, _I64, _I64, _I64, _I64, _I64, _P, i32, _P, _P, _I64, _P, _P, _P, _SZ, _P],
+        "sq_route_workspace_size": [_I64, _I64, ct.POINTER(_SZ)],
+        "sq_route_forward": [_P, i32, _I64, _I64, _I64, _P, i32, i32, i32, i32, i32, f32, _P, _P, _P, _P, _P, _SZ, _P],
+        "sq_route_backward": [_P, _P, i32, _I64, _I64, _I64, i32, i32, i32, f32, _P, _P, _P, _I64, _P],
+        "sq_exchange_dispatch": [_P, i32, _I64, _I64, _I64, _P, i32, _P, _I64, _I64, _P],
+        "sq_exchange_combine": [_P, i32, _I64, _I64, _I64, _P, _P, _I64, i32, _P, _I64, _P, _I64, _P],
+        "sq_exchange_combine_backward": [_P, _P, i32, _I64, _I64, _I64, _I64, _P, _P, _I64, i32, _P, _I64, _P, _P],
     })
     for name, args in sig.items():
         f = getattr(L, name)
