@@ -962,6 +962,102 @@ sq_status sq_exchange_combine_backward(const void* dout, const void* R, int32_t 
                                        int64_t ld_dout, int64_t ld_r, const int32_t* place, const float* share, int64_t T, int32_t k,
                                        void* dR, int64_t ld_dr, float* dshare, void* stream);
 
+/* =========================================================================
+ * Dense linear layers Y = X W^T, trained (dX = dY W, dW = dY^T X) or served, with
+ * operands in 8-bit floating point (E4M3 elements) and fp32 accumulation on the
+ * matrix cores.  One E8M0 scale for 128 consecutive elements of a product's inner
+ * axis (X and dY, along the axis of each product that they are in), or for 128 x 128
+ * elements (square: W, so that W and W^T hold the same values).
+ *
+ * A block with largest magnitude a:
+ *   s    = the smallest byte with a / 2^(s - 127) <= 464 (at least 0)
+ *   code = x / 2^(s - 127) rounded to the nearest E4M3 value (bias 7, largest 448,
+ *          below 2^-6 multiples of 2^-9), ties to the even code (464 is halfway
+ *          from 448 to the next step, so nothing is off by more than half a step);
+ *   a block that holds NaN or Inf: s = 255, which stands for NaN in all of it.
+ * Values that a code and scale stand for are exact in bf16 and fp32, but those
+ * past their range (of a block with a > 1.8125 * 2^127: Inf) and, of scales below
+ * 2^-117 (bf16) or 2^-140, those below their subnormals' step.
+ *
+ * Layout of a matrix [rows, K] (sq_f8_size bytes): rows in groups of 16, K in units
+ * of 512.  Element (r, k) is byte
+ *   ((r / 16) * units + k / 512) * 8192 + (k / 128) % 4 * 2048
+ *       + (k / 16) % 8 * 256 + (r % 16) * 16 + k % 16,
+ * its block's scale byte
+ *   ((r / 16) * units + k / 512) * 64 + (r % 16) * 4 + (k / 128) % 4.
+ * Writers fill K up to the next multiple of 128 with zeros; the rest of the padding
+ * is not written and never used.  codes must be 16-byte aligned, scales 4-byte.
+ *
+ * Sizes, SQ_ERR_INVALID_ARGUMENT otherwise: rows < 2^31; columns of values < 2^20.
+ * Inner axes of products < 2^22 (SQ_ERR_UNSUPPORTED).
+ * ========================================================================= */
+sq_status sq_f8_size(int64_t rows, int64_t cols, size_t* code_bytes, size_t* scale_bytes);
+
+/* sq_f8_quantize -- codes of X [rows, cols] in one read: codes, scales of the matrix
+ * [rows, cols] with blocks along the columns, codes_t, scales_t of the transpose
+ * [cols, rows] with blocks along the rows (either pair may be NULL, not both);
+ * square = 1: blocks of 128 x 128 in both.
+ * Errors: SQ_ERR_INVALID_ARGUMENT, SQ_ERR_UNSUPPORTED (with codes_t: rows >= 2^22),
+ * SQ_ERR_HIP. */
+sq_status sq_f8_quantize(const void* X, int32_t type, int64_t rows, int64_t cols, int64_t ld, int32_t square,
+                         uint8_t* codes, uint8_t* scales, uint8_t* codes_t, uint8_t* scales_t, void* stream);
+
+/* sq_f8_dequantize -- the values [rows, cols] of a matrix, as fp32 or bf16. */
+sq_status sq_f8_dequantize(const uint8_t* codes, const uint8_t* scales, int64_t rows, int64_t cols,
+                           void* out, int32_t type, int64_t ld, void* stream);
+
+/* sq_f8_gemm -- C [M, N] = A B^T, A [M, K], B [N, K]; C fp32, or bf16 rounded once to
+ * the nearest even.  K = 0 gives zeros.
+ * Workspace: sq_f8_gemm_workspace_size bytes (0: none), 16-byte aligned.
+ * Errors: SQ_ERR_INVALID_ARGUMENT, SQ_ERR_UNSUPPORTED, SQ_ERR_WORKSPACE_TOO_SMALL,
+ * SQ_ERR_HIP. */
+sq_status sq_f8_gemm_workspace_size(int64_t M, int64_t N, int64_t K, size_t* bytes);
+sq_status sq_f8_gemm(const uint8_t* A, const uint8_t* A_scales, const uint8_t* B, const uint8_t* B_scales,
+                     int64_t M, int64_t N, int64_t K, void* C, int32_t type, int64_t ldc,
+                     void* workspace, size_t workspace_bytes, void* stream);
+
+/* sq_f8_linear -- Y [M, N] = X W^T with X [M, K] in fp32 or bf16, quantized on the way:
+ * what sq_f8_quantize and sq_f8_gemm give.  Few rows (at most 16, more for small
+ * layers) take one launch and no workspace, the serving form for single tokens.
+ * Workspace: sq_f8_linear_workspace_size bytes (0: none), 16-byte aligned.
+ * Errors: as sq_f8_gemm. */
+sq_status sq_f8_linear_workspace_size(int64_t M, int64_t K, int64_t N, size_t* bytes);
+sq_status sq_f8_linear(const void* X, int32_t type, int64_t M, int64_t K, int64_t ld,
+                       const uint8_t* W, const uint8_t* W_scales, int64_t N, void* Y, int32_t out_type, int64_t ldy,
+                       void* workspace, size_t workspace_bytes, void* stream);
+
+/* ---------------------------------------------------------------------------
+ * sq_f8_layer -- the buffers of a linear layer that is trained, allocated once by the
+ * caller (host struct, read during the calls only), and its three steps:
+ *   sq_f8_layer_weight    codes of W [c_out, c_in] in square blocks, and of W^T, after
+ *                         each update of W
+ *   sq_f8_layer_forward   codes of X [rows, c_in] along both axes, Y = X W^T
+ *   sq_f8_layer_backward  codes of dY [rows, c_out] along both axes, then
+ *                         dX = dY W [rows, c_in] and dW = dY^T X [c_out, c_in]
+ * Each is what sq_f8_quantize and sq_f8_gemm give; dX and dW share a launch where they
+ * take the same tiles.  Y and dX have the layer's type, dW is fp32.
+ * Sizes: w [c_out, c_in], w_t [c_in, c_out], x [rows, c_in], x_t [c_in, rows],
+ * dy [rows, c_out], dy_t [c_out, rows]; every one of sq_f8_size bytes.
+ * Workspace: sq_f8_layer_workspace_size bytes (0: none), 16-byte aligned.
+ * Errors: as sq_f8_quantize and sq_f8_gemm.
+ * ------------------------------------------------------------------------- */
+typedef struct {
+    int64_t rows, c_in, c_out;
+    int32_t type;                          /* SQ_TYPE_* of X, Y, dY, dX and W */
+    int32_t reserved;                      /* 0 */
+    uint8_t *w, *w_scales, *w_t, *w_t_scales;
+    uint8_t *x, *x_scales, *x_t, *x_t_scales;
+    uint8_t *dy, *dy_scales, *dy_t, *dy_t_scales;
+    void* workspace;
+    size_t workspace_bytes;
+} sq_f8_layer;
+
+sq_status sq_f8_layer_workspace_size(const sq_f8_layer* layer, size_t* bytes);
+sq_status sq_f8_layer_weight(const sq_f8_layer* layer, const void* W, int64_t ld, void* stream);
+sq_status sq_f8_layer_forward(const sq_f8_layer* layer, const void* X, int64_t ld, void* Y, int64_t ldy, void* stream);
+sq_status sq_f8_layer_backward(const sq_f8_layer* layer, const void* dY, int64_t ld, void* dX, int64_t ld_dx,
+                               float* dW, int64_t ld_dw, void* stream);
+
 /* Static description of a status code. */
 const char* sq_status_string(sq_status s);
 

@@ -13,7 +13,8 @@ CSRC = os.path.join(HERE, "csrc")
 INCLUDE = os.path.join(ROOT, "include")
 LIB = os.path.join(HERE, "libshiftquant.so")
 SOURCES = ["sq_abi.hip", "sq_quant.hip", "sq_gemm.hip", "sq_l1bn.hip", "sq_mx_abi.hip", "sq_mx.hip",
-           "sq_mx_gemm.hip", "sq_act.hip", "sq_block_abi.hip", "sq_norm.hip", "sq_route.hip", "sq_exchange.hip"]
+           "sq_mx_gemm.hip", "sq_act.hip", "sq_block_abi.hip", "sq_norm.hip", "sq_route.hip", "sq_exchange.hip",
+           "sq_f8_abi.hip", "sq_f8.hip", "sq_f8_gemm.hip"]
 ARCH = "gfx950"
 
 HIPCC_FLAGS = [

@@ -54,6 +54,8 @@ EXPORTS = (
     "sq_mx_layer_forward", "sq_mx_layer_backward", "sq_act_size", "sq_act_forward", "sq_act_backward",
     "sq_norm_forward", "sq_norm_backward_workspace_size", "sq_norm_backward", "sq_route_workspace_size", "sq_route_forward",
     "sq_route_backward", "sq_exchange_dispatch", "sq_exchange_combine", "sq_exchange_combine_backward",
+    "sq_f8_size", "sq_f8_quantize", "sq_f8_dequantize", "sq_f8_gemm_workspace_size", "sq_f8_gemm", "sq_f8_linear_workspace_size",
+    "sq_f8_linear", "sq_f8_layer_workspace_size", "sq_f8_layer_weight", "sq_f8_layer_forward", "sq_f8_layer_backward",
     "sq_status_string", "sq_last_error", "sq_last_error_string",
 )
 
@@ -203,6 +205,19 @@ def load() -> ct.CDLL:
         "sq_exchange_dispatch": [_P, i32, _I64, _I64, _I64, _P, i32, _P, _I64, _I64, _P],
         "sq_exchange_combine": [_P, i32, _I64, _I64, _I64, _P, _P, _I64, i32, _P, _I64, _P, _I64, _P],
         "sq_exchange_combine_backward": [_P, _P, i32, _I64, _I64, _I64, _I64, _P, _P, _I64, i32, _P, _I64, _P, _P],
+    })
+    sig.update({   # wrapped in the f8 module
+        "sq_f8_size": [_I64, _I64, ct.POINTER(_SZ), ct.POINTER(_SZ)],
+        "sq_f8_quantize": [_P, i32, _I64, _I64, _I64, i32, _P, _P, _P, _P, _P],
+        "sq_f8_dequantize": [_P, _P, _I64, _I64, _P, i32, _I64, _P],
+        "sq_f8_gemm_workspace_size": [_I64, _I64, _I64, ct.POINTER(_SZ)],
+        "sq_f8_gemm": [_P, _P, _P, _P, _I64, _I64, _I64, _P, i32, _I64, _P, _SZ, _P],
+        "sq_f8_linear_workspace_size": [_I64, _I64, _I64, ct.POINTER(_SZ)],
+        "sq_f8_linear": [_P, i32, _I64, _I64, _I64, _P, _P, _I64, _P, i32, _I64, _P, _SZ, _P],
+        "sq_f8_layer_workspace_size": [_P, ct.POINTER(_SZ)],
+        "sq_f8_layer_weight": [_P, _P, _I64, _P],
+        "sq_f8_layer_forward": [_P, _P, _I64, _P, _I64, _P],
+        "sq_f8_layer_backward": [_P, _P, _I64, _P, _I64, _P, _I64, _P],
     })
     for name, args in sig.items():
         f = getattr(L, name)
