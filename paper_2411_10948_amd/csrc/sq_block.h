@@ -40,12 +40,13 @@ struct RouteArgs {
     float* share;                       // [T, k]
     int32_t *chosen, *place;            // [T, k]
     int32_t* offsets;                   // [E + 1]
-    uint8_t* counts;                    // [blocks, E] rows of a block by expert
+    uint8_t* counts;                    // [blocks, route_stride(E)] rows of a block by expert
     int32_t* base;                      // [blocks + 1, E]: rows before the block's by expert; last row: all
     const float* dshare;                // backward
     void* dlogits;
     int64_t ld_d;
 };
+__host__ __device__ inline int64_t route_stride(int64_t E) { return (E + 3) / 4 * 4; }     // whole words
 inline int64_t route_blocks(int64_t T) { return (T + kRouteTokens - 1) / kRouteTokens; }
 hipError_t launch_route_forward(const RouteArgs& a, hipStream_t s);
 hipError_t launch_route_backward(const RouteArgs& a, hipStream_t s);

@@ -57,7 +57,7 @@ RouteWorkspace route_workspace(int64_t T, int64_t E) {
     RouteWorkspace w;
     const int64_t blocks = route_blocks(T);
     if (blocks <= 1) return w;
-    w.counts = (size_t)round_up(blocks * E, 256);
+    w.counts = (size_t)round_up(blocks * route_stride(E), 256);
     w.base = (size_t)round_up((blocks + 1) * E * 4, 256);
     return w;
 }

@@ -105,6 +105,19 @@ def test_ties_go_to_the_lowest_index(route, groups, top_groups, score):
         _check(route, _cuda(logits), k, score, bias, groups, top_groups, renorm=True)
 
 
+@pytest.mark.parametrize("k", [1, 8, 14, 15, 16, 20])
+@pytest.mark.parametrize("score", ["softmax", "sigmoid"])
+@pytest.mark.parametrize("groups", [1, 4])
+def test_sums_that_fp32_cannot_tell_apart(route, score, groups, k):
+    # experts an ulp of their logits apart, in runs of equal and of nearly equal ones, under biases that hide it in fp32
+    rng = np.random.default_rng(k)
+    step = np.float32(0.5) + rng.integers(0, 40, (60, 96)) * np.float32(2.0 ** -24)
+    for bias in (np.full(96, 0.75), np.zeros(96), np.repeat([1.0, -1.0, 0.5], 32)):
+        _check(route, _cuda(step), k, score, bias, groups, groups, renorm=True)
+    step[:, ::3] = rng.standard_normal((60, 32))
+    _check(route, _cuda(step), k, score, 0.1 * rng.standard_normal(96), groups, max(1, groups - 1))
+
+
 @pytest.mark.parametrize("E,k", [(1, 1), (5, 5), (64, 64), (65, 64), (1024, 64)])
 def test_every_expert_chosen(route, E, k):
     _check(route, _cuda(np.random.default_rng(E).standard_normal((70, E))), k, renorm=True)
