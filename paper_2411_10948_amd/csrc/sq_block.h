@@ -76,11 +76,15 @@ hipError_t launch_combine_backward(const ExchangeArgs& a, hipStream_t s);
 template <typename T>
 constexpr int kVec = 16 / (int)sizeof(T);       // elements of a 16-byte piece
 
-// 16 bytes of a row from column c as they came; columns at and past `cols` read as zero.
-template <typename T>
-__device__ __forceinline__ void load16(const T* row, int64_t c, int64_t cols, uint32_t* w) {
-    if (c + kVec<T> <= cols) {
-        const u32x4_any v = *reinterpret_cast<const u32x4_any*>(row + c);
+// 16 bytes of a row from column c < cols as they came; columns at and past `cols`
+// read as zero.  WHOLE: there are none, rows are whole pieces.  NT: past the caches.
+template <bool WHOLE = false, bool NT = false, typename T>
+__device__ __forceinline__ void load16(const T* row, int c, int cols, uint32_t* w) {
+    if (WHOLE || c + kVec<T> <= cols) {
+        const u32x4_any* at = reinterpret_cast<const u32x4_any*>(row + (uint32_t)c);
+        u32x4_any v;
+        if constexpr (NT) v = __builtin_nontemporal_load(at);
+        else v = *at;
         w[0] = v.x;
         w[1] = v.y;
         w[2] = v.z;
@@ -88,22 +92,24 @@ __device__ __forceinline__ void load16(const T* row, int64_t c, int64_t cols, ui
     } else {
         T t[kVec<T>];       // loads without branches, those past the end cleared
 #pragma unroll
-        for (int e = 0; e < kVec<T>; ++e) t[e] = row[min(c + e, cols - 1)];
+        for (int e = 0; e < kVec<T>; ++e) t[e] = row[(uint32_t)min(c + e, cols - 1)];
 #pragma unroll
         for (int e = 0; e < kVec<T>; ++e) t[e] = c + e < cols ? t[e] : (T)0;
         __builtin_memcpy(w, t, 16);
     }
 }
-template <typename T>
-__device__ __forceinline__ void store16(T* row, int64_t c, int64_t cols, const uint32_t* w) {
-    if (c + kVec<T> <= cols) {
-        *reinterpret_cast<u32x4_any*>(row + c) = u32x4_any{w[0], w[1], w[2], w[3]};
+template <bool WHOLE = false, bool NT = false, typename T>
+__device__ __forceinline__ void store16(T* row, int c, int cols, const uint32_t* w) {
+    if (WHOLE || c + kVec<T> <= cols) {
+        u32x4_any* to = reinterpret_cast<u32x4_any*>(row + (uint32_t)c);
+        if constexpr (NT) __builtin_nontemporal_store(u32x4_any{w[0], w[1], w[2], w[3]}, to);
+        else *to = u32x4_any{w[0], w[1], w[2], w[3]};
     } else {
         T t[kVec<T>];
         __builtin_memcpy(t, w, 16);
 #pragma unroll
         for (int e = 0; e < kVec<T>; ++e)
-            if (c + e < cols) row[c + e] = t[e];
+            if (c + e < cols) row[(uint32_t)(c + e)] = t[e];
     }
 }
 // fp32 values of a piece, and back (rounded once to bf16)
@@ -173,6 +179,20 @@ __device__ __forceinline__ F wave_max(F v) {
     v = larger(v, wave_move<0x142, 0xA>(v, v));
     v = larger(v, wave_move<0x143, 0xC>(v, v));
     return wave_lane(v, 63);
+}
+template <int CTRL, typename F>
+__device__ __forceinline__ F row_move(F v) {
+    return wave_move<CTRL, 0xF>(v, v);
+}
+constexpr int kLane1 = 0xB1, kLane2 = 0x4E, kMirror8 = 0x141, kMirror16 = 0x140;     // partners in a sum over 2, 4, 8, 16 lanes
+// f over the `lanes` lanes (1, 2, 4, 8 or 16) that start at a multiple of it
+template <typename F, class Op>
+__device__ __forceinline__ F over_lanes(F v, int lanes, Op op) {
+    if (lanes > 1) v = op(v, row_move<kLane1>(v));
+    if (lanes > 2) v = op(v, row_move<kLane2>(v));
+    if (lanes > 4) v = op(v, row_move<kMirror8>(v));
+    if (lanes > 8) v = op(v, row_move<kMirror16>(v));
+    return v;
 }
 #endif
 

@@ -265,20 +265,6 @@ __global__ __launch_bounds__(1024) void k_route(RouteArgs p) {
 // Scores and sums with biases are fp32 here; where these leave the order in doubt
 // (EXACT) the token is done again by the whole wave in fp64.
 // ---------------------------------------------------------------------------
-template <int CTRL, typename F>
-__device__ __forceinline__ F row_move(F v) {
-    return wave_move<CTRL, 0xF>(v, v);
-}
-constexpr int kLane1 = 0xB1, kLane2 = 0x4E, kMirror8 = 0x141, kMirror16 = 0x140;     // partners in a sum over 2, 4, 8, 16 lanes
-// f over the `lanes` lanes (1, 2, 4, 8 or 16) that start at a multiple of it
-template <typename F, class Op>
-__device__ __forceinline__ F over_lanes(F v, int lanes, Op op) {
-    if (lanes > 1) v = op(v, row_move<kLane1>(v));
-    if (lanes > 2) v = op(v, row_move<kLane2>(v));
-    if (lanes > 4) v = op(v, row_move<kMirror8>(v));
-    if (lanes > 8) v = op(v, row_move<kMirror16>(v));
-    return v;
-}
 template <typename F>
 __device__ __forceinline__ F max16(F v) {
     return over_lanes(v, 16, [](F a, F b) { return larger(a, b); });
