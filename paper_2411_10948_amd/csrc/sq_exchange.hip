@@ -9,6 +9,7 @@
 // product is 0.  Each row is read or written once; bound by HBM, small calls by
 // their one launch.
 #include <algorithm>
+#include <type_traits>
 
 #include "sq_block.h"
 
@@ -17,7 +18,7 @@ namespace sq {
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int kSlots = 8;       // rows in flight a thread
+constexpr int kMostSlots = 8;   // rows in flight a thread
 
 constexpr int64_t kMaxGrid = 1 << 20;   // blocks along the tokens; more of them take turns
 
@@ -30,19 +31,19 @@ __device__ __forceinline__ void my_pieces(const ExchangeArgs& p, int tpr, F f) {
     for (int64_t t = blockIdx.x * per + threadIdx.x / tpr; t < p.T; t += gridDim.x * per) f(t, c);
 }
 
-template <typename T>
+template <typename T, bool NT>
 __global__ __launch_bounds__(kThreads) void k_dispatch(ExchangeArgs p, int tpr) {
     my_pieces<T>(p, tpr, [&](int64_t t, int64_t c) {
         uint32_t w[4];
         load16(static_cast<const T*>(p.x) + t * p.ld_x, c, p.D, w);
         for (int j = 0; j < p.k; ++j) {
             const uint32_t at = (uint32_t)p.place[t * p.k + j];
-            if (at < (uint64_t)p.rows) store16(static_cast<T*>(p.rows_out) + at * p.ld_rows, c, p.D, w);
+            if (at < (uint64_t)p.rows) store16<false, NT>(static_cast<T*>(p.rows_out) + at * p.ld_rows, c, p.D, w);
         }
     });
 }
 
-template <typename T, bool SHARES>
+template <typename T, bool SHARES, int kSlots, bool NT>
 __global__ __launch_bounds__(kThreads) void k_combine(ExchangeArgs p, int tpr) {
     constexpr int N = kVec<T>;
     my_pieces<T>(p, tpr, [&](int64_t t, int64_t c) {
@@ -66,7 +67,7 @@ __global__ __launch_bounds__(kThreads) void k_combine(ExchangeArgs p, int tpr) {
                 const uint32_t at = (uint32_t)p.place[t * p.k + j0 + j];
                 if (at >= (uint64_t)p.rows) continue;
                 share[j] = SHARES ? p.share[t * p.k + j0 + j] : 1.0f;
-                load16(static_cast<const T*>(p.rows_in) + at * p.ld_in, c, p.D, w[j]);
+                load16<false, NT>(static_cast<const T*>(p.rows_in) + at * p.ld_in, c, p.D, w[j]);
             }
 #pragma unroll
             for (int j = 0; j < kSlots; ++j) {
@@ -78,13 +79,13 @@ __global__ __launch_bounds__(kThreads) void k_combine(ExchangeArgs p, int tpr) {
         }
         uint32_t w[4];
         pack16<T>(sum, w);
-        store16(static_cast<T*>(p.out) + t * p.ld_out, c, p.D, w);
+        store16<false, NT>(static_cast<T*>(p.out) + t * p.ld_out, c, p.D, w);
     });
 }
 
 // WAVES waves a token; the products' sums over a wave's pieces, its lanes and the
 // waves, in that order.
-template <typename T, int WAVES>
+template <typename T, int WAVES, int kSlots, bool NT>
 __global__ __launch_bounds__(kThreads) void k_combine_backward(ExchangeArgs p) {
     constexpr int N = kVec<T>, TPR = 64 * WAVES;
     __shared__ float sums[kThreads / 64][kSlots];
@@ -108,7 +109,7 @@ __global__ __launch_bounds__(kThreads) void k_combine_backward(ExchangeArgs p) {
                 load16(static_cast<const T*>(p.x) + t * p.ld_x, c, p.D, d);
 #pragma unroll
                 for (int j = 0; j < kSlots; ++j)
-                    if (at[j] < (uint64_t)p.rows) load16(static_cast<const T*>(p.rows_in) + at[j] * p.ld_in, c, p.D, y[j]);
+                    if (at[j] < (uint64_t)p.rows) load16<false, NT>(static_cast<const T*>(p.rows_in) + at[j] * p.ld_in, c, p.D, y[j]);
                 float df[N];
                 values16<T>(d, df);
 #pragma unroll
@@ -122,7 +123,7 @@ __global__ __launch_bounds__(kThreads) void k_combine_backward(ExchangeArgs p) {
                         o[e] = share[j] * df[e];
                     }
                     pack16<T>(o, y[j]);
-                    store16(static_cast<T*>(p.rows_out) + at[j] * p.ld_rows, c, p.D, y[j]);
+                    store16<false, NT>(static_cast<T*>(p.rows_out) + at[j] * p.ld_rows, c, p.D, y[j]);
                 }
             }
 #pragma unroll
@@ -151,27 +152,48 @@ dim3 grid_of(int64_t T_, int64_t D, int& tpr) {
     return dim3((uint32_t)std::min<int64_t>((T_ + kThreads / tpr - 1) / (kThreads / tpr), kMaxGrid), (uint32_t)((n + tpr - 1) / tpr));
 }
 
+// f(slots in flight, whether the rows go past the caches) as compile-time constants
+template <typename T, class F>
+hipError_t with_rows(const ExchangeArgs& a, F f) {
+    const bool nt = (double)a.T * a.k * (double)a.D * sizeof(T) >= 32e6;
+    const auto slots = [&](auto NT) {
+        if (a.k <= 2) return f(std::integral_constant<int, 2>(), NT);
+        if (a.k <= 4) return f(std::integral_constant<int, 4>(), NT);
+        return f(std::integral_constant<int, kMostSlots>(), NT);
+    };
+    return nt ? slots(std::true_type()) : slots(std::false_type());
+}
+
 template <typename T>
 hipError_t dispatch(const ExchangeArgs& a, hipStream_t s) {
     int tpr;
     const dim3 grid = grid_of<T>(a.T, a.D, tpr);
-    k_dispatch<T><<<grid, kThreads, 0, s>>>(a, tpr);
-    return hipGetLastError();
+    return with_rows<T>(a, [&](auto, auto NT) {
+        k_dispatch<T, decltype(NT)::value><<<grid, kThreads, 0, s>>>(a, tpr);
+        return hipGetLastError();
+    });
 }
 template <typename T>
 hipError_t combine(const ExchangeArgs& a, hipStream_t s) {
     int tpr;
     const dim3 grid = grid_of<T>(a.T, a.D, tpr);
-    if (a.share) k_combine<T, true><<<grid, kThreads, 0, s>>>(a, tpr);
-    else k_combine<T, false><<<grid, kThreads, 0, s>>>(a, tpr);
-    return hipGetLastError();
+    return with_rows<T>(a, [&](auto SLOTS, auto NT) {
+        constexpr int slots = decltype(SLOTS)::value;
+        if (a.share) k_combine<T, true, slots, decltype(NT)::value><<<grid, kThreads, 0, s>>>(a, tpr);
+        else k_combine<T, false, slots, decltype(NT)::value><<<grid, kThreads, 0, s>>>(a, tpr);
+        return hipGetLastError();
+    });
 }
 template <typename T>
 hipError_t combine_backward(const ExchangeArgs& a, hipStream_t s) {
     const int64_t n = (a.D + kVec<T> - 1) / kVec<T>;
-    if (n <= 64) k_combine_backward<T, 1><<<(uint32_t)std::min<int64_t>((a.T + 3) / 4, kMaxGrid), kThreads, 0, s>>>(a);
-    else k_combine_backward<T, 4><<<(uint32_t)std::min<int64_t>(a.T, kMaxGrid), kThreads, 0, s>>>(a);
-    return hipGetLastError();
+    return with_rows<T>(a, [&](auto SLOTS, auto NT) {
+        constexpr int slots = decltype(SLOTS)::value;
+        constexpr bool nt = decltype(NT)::value;
+        if (n <= 64) k_combine_backward<T, 1, slots, nt><<<(uint32_t)std::min<int64_t>((a.T + 3) / 4, kMaxGrid), kThreads, 0, s>>>(a);
+        else k_combine_backward<T, 4, slots, nt><<<(uint32_t)std::min<int64_t>(a.T, kMaxGrid), kThreads, 0, s>>>(a);
+        return hipGetLastError();
+    });
 }
 
 }  // namespace
