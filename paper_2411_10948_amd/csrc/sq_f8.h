@@ -42,7 +42,7 @@ struct F8GemmArgs {
     int64_t ldc;
     float* part;                        // split-K partials [splits, M, N]
 };
-int64_t f8_gemm_splits(int64_t M, int64_t N, int64_t K);
+int64_t f8_gemm_splits(int64_t M, int64_t N, int64_t K, int type);      // type of the result
 hipError_t launch_f8_gemm(const F8GemmArgs& a, hipStream_t s);
 // Both products, in one launch where they take the same tiles; their partials must not overlap.
 hipError_t launch_f8_gemm_pair(const F8GemmArgs& a, const F8GemmArgs& b, hipStream_t s);

@@ -19,8 +19,8 @@ sq_status check_f8_inner(int64_t k) {
     return SQ_OK;
 }
 
-size_t f8_part_bytes(int64_t M, int64_t N, int64_t K) {
-    const int64_t s = M && N ? f8_gemm_splits(M, N, K) : 1;
+size_t f8_part_bytes(int64_t M, int64_t N, int64_t K, int32_t type) {
+    const int64_t s = M && N ? f8_gemm_splits(M, N, K, type) : 1;
     return s > 1 ? (size_t)round_up(s * M * N * 4, 256) : 0;
 }
 
@@ -44,12 +44,12 @@ struct F8Workspace {
     size_t codes = 0, scales = 0, part = 0;
     size_t bytes() const { return codes + scales + part; }
 };
-F8Workspace f8_workspace(int64_t M, int64_t K, int64_t N, int type) {
+F8Workspace f8_workspace(int64_t M, int64_t K, int64_t N, int32_t type, int32_t out_type) {
     F8Workspace w;
     if (M == 0 || N == 0 || f8_rows_ok(M, K, N, type)) return w;
     w.codes = (size_t)round_up(f8_code_bytes(M, K), 256);
     w.scales = (size_t)round_up(f8_scale_bytes(M, K), 256);
-    w.part = f8_part_bytes(M, N, K);
+    w.part = f8_part_bytes(M, N, K, out_type);
     return w;
 }
 
@@ -80,8 +80,8 @@ sq_status check_f8_layer(const sq_f8_layer* l) {
 }
 
 size_t f8_layer_workspace(const sq_f8_layer* l) {
-    return std::max(f8_part_bytes(l->rows, l->c_out, l->c_in),
-                    f8_part_bytes(l->rows, l->c_in, l->c_out) + f8_part_bytes(l->c_out, l->c_in, l->rows));
+    return std::max(f8_part_bytes(l->rows, l->c_out, l->c_in, l->type),
+                    f8_part_bytes(l->rows, l->c_in, l->c_out, l->type) + f8_part_bytes(l->c_out, l->c_in, l->rows, SQ_TYPE_F32));
 }
 
 }  // namespace
@@ -149,7 +149,7 @@ sq_status sq_f8_gemm_workspace_size(int64_t M, int64_t N, int64_t K, size_t* byt
     return guarded([&]() -> sq_status {
         SQ_TRY(check_f8_product(M, N, K));
         if (!bytes) return invalid("bytes is NULL");
-        *bytes = f8_part_bytes(M, N, K);
+        *bytes = std::max(f8_part_bytes(M, N, K, SQ_TYPE_F32), f8_part_bytes(M, N, K, SQ_TYPE_BF16));
         return SQ_OK;
     });
 }
@@ -165,7 +165,7 @@ sq_status sq_f8_gemm(const uint8_t* A, const uint8_t* A_scales, const uint8_t* B
             SQ_TRY(check_mx(B, B_scales, "B"));
         }
         SQ_TRY(check_values(C, type, ldc, N, "C"));
-        SQ_TRY(check_workspace(workspace, workspace_bytes, f8_part_bytes(M, N, K)));
+        SQ_TRY(check_workspace(workspace, workspace_bytes, f8_part_bytes(M, N, K, type)));
         return hip_status(launch_f8_gemm(product_args(A, A_scales, B, B_scales, M, N, K, C, type, ldc, workspace),
                                          static_cast<hipStream_t>(stream)), "f8 gemm");
     });
@@ -175,7 +175,10 @@ sq_status sq_f8_linear_workspace_size(int64_t M, int64_t K, int64_t N, size_t* b
     return guarded([&]() -> sq_status {
         SQ_TRY(check_f8_linear(M, N, K));
         if (!bytes) return invalid("bytes is NULL");
-        *bytes = std::max(f8_workspace(M, K, N, SQ_TYPE_F32).bytes(), f8_workspace(M, K, N, SQ_TYPE_BF16).bytes());
+        *bytes = 0;
+        for (const int32_t type : {SQ_TYPE_F32, SQ_TYPE_BF16})
+            for (const int32_t out_type : {SQ_TYPE_F32, SQ_TYPE_BF16})
+                *bytes = std::max(*bytes, f8_workspace(M, K, N, type, out_type).bytes());
         return SQ_OK;
     });
 }
@@ -192,7 +195,7 @@ sq_status sq_f8_linear(const void* X, int32_t type, int64_t M, int64_t K, int64_
             SQ_TRY(check_mx(W, W_scales, "W"));
         }
         SQ_TRY(check_values(Y, out_type, ldy, N, "Y"));
-        const F8Workspace w = f8_workspace(M, K, N, type);
+        const F8Workspace w = f8_workspace(M, K, N, type, out_type);
         SQ_TRY(check_workspace(workspace, workspace_bytes, w.bytes()));
         hipStream_t s = static_cast<hipStream_t>(stream);
         if (f8_rows_ok(M, K, N, type)) {
@@ -277,7 +280,7 @@ sq_status sq_f8_layer_backward(const sq_f8_layer* layer, const void* dY, int64_t
         }
         SQ_TRY(check_workspace(l.workspace, l.workspace_bytes, f8_layer_workspace(layer)));
         SQ_TRY(sq_f8_quantize(dY, l.type, l.rows, l.c_out, ld, 0, l.dy, l.dy_scales, l.dy_t, l.dy_t_scales, stream));
-        const size_t part = f8_part_bytes(l.rows, l.c_in, l.c_out);
+        const size_t part = f8_part_bytes(l.rows, l.c_in, l.c_out, l.type);
         const F8GemmArgs x = product_args(l.dy, l.dy_scales, l.w_t, l.w_t_scales, l.rows, l.c_in, l.c_out, dX, l.type, ld_dx,
                                           l.workspace),
                          w = product_args(l.dy_t, l.dy_t_scales, l.x_t, l.x_t_scales, l.c_out, l.c_in, l.rows, dW, SQ_TYPE_F32,

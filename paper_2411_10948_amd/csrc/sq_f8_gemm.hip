@@ -60,8 +60,8 @@ __device__ __forceinline__ void wait_loads() {
     __builtin_amdgcn_s_waitcnt((N & 0xF) | ((N >> 4) << 14) | (0x7 << 4));
 }
 
-// Block tile BM x BN of WM x WN waves, a ring of STAGES stages of 64 inner elements
-// in LDS; a stage's operands are read into registers while the one before is
+// Block tile BM x BN of WM x WN waves, a ring of STAGES stages of half a tile (64 inner
+// elements) in LDS; operands are read into registers while those before them are
 // multiplied.
 template <int BM_, int BN_, int WM_, int WN_, int STAGES_, int BLOCKS>
 struct F8Cfg {
@@ -74,11 +74,11 @@ struct F8Cfg {
     static constexpr int kCols = TN < 64 ? TN : 64;           // columns of the epilogue's pieces
     static constexpr int kLd = kCols + 4;
     static constexpr int kSmem = std::max(STAGES * kStage, kWaves * 32 * kLd * 4);
-    static constexpr int kCycle = 16;                         // half tiles after which stage, scale buffer and scale byte recur
+    static constexpr int kCycle = 8;                          // stages of a unit: scale bytes are part of the instruction
     static_assert(BM / 16 % kWaves == 0 && BN / 16 % kWaves == 0, "a wave's i-th loads are all of A or all of B");
-    static_assert(kCycle % STAGES == 0 && BLOCKS * kSmem <= 160 * 1024, "ring");
+    static_assert(STAGES >= 3 && BLOCKS * kSmem <= 160 * 1024, "ring");
 };
-using F8Wide = F8Cfg<256, 256, 4, 2, 4, 1>;     // waves of 64 x 128
+using F8Wide = F8Cfg<128, 256, 2, 2, 3, 2>;     // waves of 64 x 128
 using F8Mid = F8Cfg<128, 128, 2, 2, 4, 2>;      // waves of 64 x 64
 using F8Small = F8Cfg<64, 64, 2, 2, 4, 4>;      // waves of 32 x 32
 
@@ -108,6 +108,8 @@ __device__ __forceinline__ void unrolled_steps(F f) {
         if (f(std::integral_constant<int, I>())) unrolled_steps<N, I + 1>(f);
     }
 }
+
+constexpr int64_t kSplit = 20, kSplitExact = 16;
 
 // A product, its tiles and K splits, and how many blocks it takes.
 struct F8Product {
@@ -151,7 +153,7 @@ __device__ __forceinline__ void product(const F8Product& d, uint32_t block, uint
                                  rAs = f8_rsrc(p.As + (m0 >> 4) * sbytes, (last_a + 1) * sbytes),
                                  rBs = f8_rsrc(p.Bs + (n0 >> 4) * sbytes, (last_b + 1) * sbytes);
     const uint32_t gb = (uint32_t)gbytes, gs = (uint32_t)sbytes;
-    // Half tiles past the last one read it again (never multiplied), so that every
+    // Stages past the last one read it again (never multiplied), so that every
     // step issues the same loads and the waits below are fixed counts.
     const int n = 2 * (int)n_tiles;
     auto issue = [&](int t, int stage) {
@@ -173,145 +175,161 @@ __device__ __forceinline__ void product(const F8Product& d, uint32_t block, uint
         for (int j = 0; j < T::FN; ++j)
 #pragma unroll
             for (int e = 0; e < 16; ++e) acc[i][j][e] = 0.0f;
-    // The scales of four tiles, one word a lane's row; two buffers.
-    int sa[2][T::FM], sb[2][T::FN];
+    // The scales of a unit, one word a lane's row, and those of the next one on their way.
+    int sa[T::FM], sb[T::FN], na[T::FM], nb[T::FN];
     const uint32_t row16 = ((uint32_t)lane & 15u) * 4u;
     const int upper = (lane >> 4) & 1;      // which 16-row group of a fragment's two
-    auto load_scales = [&](int unit, auto BUF) {
-        constexpr int buf = decltype(BUF)::value;
+    auto load_scales = [&](int unit) {
         const int k = ((int)(t0 >> 2) + min(unit, (n - 1) >> 3)) * kF8UnitScales;
 #pragma unroll
         for (int i = 0; i < T::FM; ++i)
-            sa[buf][i] = (int)__builtin_amdgcn_raw_buffer_load_b32(
+            na[i] = (int)__builtin_amdgcn_raw_buffer_load_b32(
                 rAs, row16 + (uint32_t)min(wm * T::TM / 16 + 2 * i + upper, last_a) * gs, k, 0);
 #pragma unroll
         for (int j = 0; j < T::FN; ++j)
-            sb[buf][j] = (int)__builtin_amdgcn_raw_buffer_load_b32(
+            nb[j] = (int)__builtin_amdgcn_raw_buffer_load_b32(
                 rBs, row16 + (uint32_t)min(wn * T::TN / 16 + 2 * j + upper, last_b) * gs, k, 0);
     };
-    // lane l: row l % 32, 16-element pieces 2 (l / 32) and 2 (l / 32) + 1 of the half tile
+    // lane l: row l % 32, 16-element pieces 2 (l / 32) and 2 (l / 32) + 1 of a half tile
     const uint32_t frag = (uint32_t)upper * kF8HalfBytes + ((uint32_t)lane >> 5) * 512u + ((uint32_t)lane & 15u) * 16u;
+    auto next_unit = [&]() {
+#pragma unroll
+        for (int i = 0; i < T::FM; ++i) sa[i] = na[i];
+#pragma unroll
+        for (int j = 0; j < T::FN; ++j) sb[j] = nb[j];
+    };
     auto piece_a = [&](int stg, int i, int piece) {
         return *reinterpret_cast<const v4i*>(smem + stg * T::kStage + frag + (wm * T::TM / 16 + 2 * i) * kF8HalfBytes + piece * 256);
     };
     auto piece_b = [&](int stg, int j, int piece) {
-        return *reinterpret_cast<const v4i*>(smem + stg * T::kStage + frag + (T::BM / 16 + wn * T::TN / 16 + 2 * j) * kF8HalfBytes + piece * 256);
+        return *reinterpret_cast<const v4i*>(smem + stg * T::kStage + frag + (T::BM / 16 + wn * T::TN / 16 + 2 * j) * kF8HalfBytes +
+                                             piece * 256);
     };
-    if constexpr (!EXACT) {
-        v8i fa[2][T::FM], fb[2][T::FN];
-        auto read_frags = [&](auto STG, auto BUF) {
-            constexpr int stg = decltype(STG)::value, buf = decltype(BUF)::value;
+    // Operands of the 8-bit instructions, a half tile of them, two buffers; up and down the
+    // rows of fragments: never do both operands change, which takes less power.
+    v8i fa[2][T::FM], fb[2][T::FN];
+    auto read_stage = [&](int stg, auto BUF) {
+        constexpr int buf = decltype(BUF)::value;
 #pragma unroll
-            for (int i = 0; i < T::FM; ++i) fa[buf][i] = join(piece_a(stg, i, 0), piece_a(stg, i, 1));
+        for (int i = 0; i < T::FM; ++i) fa[buf][i] = join(piece_a(stg, i, 0), piece_a(stg, i, 1));
 #pragma unroll
-            for (int j = 0; j < T::FN; ++j) fb[buf][j] = join(piece_b(stg, j, 0), piece_b(stg, j, 1));
-        };
-        // Up and down the rows of fragments: never do both operands change, which takes less power.
-        auto multiply = [&](auto S, auto BUF) {
-            constexpr int s = decltype(S)::value, buf = decltype(BUF)::value, grp = (s >> 3) & 1;
+        for (int j = 0; j < T::FN; ++j) fb[buf][j] = join(piece_b(stg, j, 0), piece_b(stg, j, 1));
+    };
+    auto multiply_stage = [&](auto S, auto BUF) {
+        constexpr int s = decltype(S)::value, buf = decltype(BUF)::value;
 #pragma unroll
-            for (int j = 0; j < T::FN; ++j)
+        for (int j = 0; j < T::FN; ++j)
+#pragma unroll
+            for (int q = 0; q < T::FM; ++q) {
+                const int i = j & 1 ? T::FM - 1 - q : q;
+                acc[i][j] = mfma32<(s >> 1)>(fb[buf][j], fa[buf][i], acc[i][j], sb[j], sa[i]);
+            }
+    };
+    // And of the bf16 ones, 16 bytes a lane of a half tile, two buffers.  One fragment a wave: two
+    // sums of its own, so that an instruction does not wait for the one before.
+    constexpr bool TWO = EXACT && T::FM * T::FN == 1;
+    v16f other;
+#pragma unroll
+    for (int e = 0; e < 16; ++e) other[e] = 0.0f;
+    v4i pa[2][T::FM], pb[2][T::FN];
+    float va[T::FM], vb[T::FN];     // the tile's scales
+    auto read_piece = [&](int stg, auto PIECE) {
+        constexpr int piece = decltype(PIECE)::value;
+#pragma unroll
+        for (int i = 0; i < T::FM; ++i) pa[piece][i] = piece_a(stg, i, piece);
+#pragma unroll
+        for (int j = 0; j < T::FN; ++j) pb[piece][j] = piece_b(stg, j, piece);
+    };
+    auto multiply_piece = [&](auto PIECE) {
+        constexpr int buf = decltype(PIECE)::value;
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            v8bf xa[T::FM];
+#pragma unroll
+            for (int i = 0; i < T::FM; ++i) xa[i] = values8(pa[buf][i][2 * h], pa[buf][i][2 * h + 1], va[i]);
+#pragma unroll
+            for (int j = 0; j < T::FN; ++j) {
+                const v8bf xb = values8(pb[buf][j][2 * h], pb[buf][j][2 * h + 1], vb[j]);
 #pragma unroll
                 for (int q = 0; q < T::FM; ++q) {
                     const int i = j & 1 ? T::FM - 1 - q : q;
-                    acc[i][j] = mfma32<((s >> 1) & 3)>(fb[buf][j], fa[buf][i], acc[i][j], sb[grp][j], sa[grp][i]);
-                }
-        };
-        // Step t, of index S in the cycle: stage t + 1 is there; refill stage t's place (its
-        // operands were read in the step before), read stage t + 1's, multiply stage t's.
-        auto step = [&](int t, auto S) {
-            constexpr int s = decltype(S)::value, buf = s & 1;
-            wait_loads<(T::STAGES - 2) * T::LPW>();
-            __builtin_amdgcn_s_barrier();
-            if constexpr ((s & 7) == 0) load_scales((t >> 3) + 1, std::integral_constant<int, ((s >> 3) & 1) ^ 1>());
-            issue(t + T::STAGES, s % T::STAGES);
-            read_frags(std::integral_constant<int, (s + 1) % T::STAGES>(), std::integral_constant<int, buf ^ 1>());
-            multiply(S, std::integral_constant<int, buf>());
-            constexpr int kReads = 2 * (T::FM + T::FN), kMfma = T::FM * T::FN, kPer = (kReads + kMfma - 1) / kMfma;
-#pragma unroll
-            for (int g = 0; g < kMfma; ++g) {
-                __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);          // an MFMA
-                __builtin_amdgcn_sched_group_barrier(0x100, kPer, 0);       // LDS reads
-            }
-        };
-        if (n > 0) {
-            load_scales(0, std::integral_constant<int, 0>());
-#pragma unroll
-            for (int i = 0; i < T::STAGES; ++i) issue(i, i);
-            wait_loads<(T::STAGES - 1) * T::LPW>();
-            __builtin_amdgcn_s_barrier();
-            read_frags(std::integral_constant<int, 0>(), std::integral_constant<int, 0>());
-            for (int t = 0; t < n; t += T::kCycle)
-                unrolled_steps<T::kCycle>([&](auto S) {
-                    constexpr int s = decltype(S)::value;
-                    if (t + s >= n) return false;
-                    step(t + s, S);
-                    return true;
-                });
-        }
-    } else {
-        v4i pa[2][T::FM], pb[2][T::FN];
-        float va[T::FM], vb[T::FN];     // the tile's scales
-        auto read_piece = [&](auto STG, auto PIECE) {
-            constexpr int stg = decltype(STG)::value, piece = decltype(PIECE)::value;
-#pragma unroll
-            for (int i = 0; i < T::FM; ++i) pa[piece][i] = piece_a(stg, i, piece);
-#pragma unroll
-            for (int j = 0; j < T::FN; ++j) pb[piece][j] = piece_b(stg, j, piece);
-        };
-        auto multiply = [&](auto PIECE) {
-            constexpr int piece = decltype(PIECE)::value;
-#pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                v8bf xa[T::FM];
-#pragma unroll
-                for (int i = 0; i < T::FM; ++i) xa[i] = values8(pa[piece][i][2 * h], pa[piece][i][2 * h + 1], va[i]);
-#pragma unroll
-                for (int j = 0; j < T::FN; ++j) {
-                    const v8bf xb = values8(pb[piece][j][2 * h], pb[piece][j][2 * h + 1], vb[j]);
-#pragma unroll
-                    for (int q = 0; q < T::FM; ++q) {
-                        const int i = j & 1 ? T::FM - 1 - q : q;
-                        acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(xb, xa[i], acc[i][j], 0, 0, 0);
-                    }
+                    v16f& to = TWO && h ? other : acc[i][j];
+                    to = __builtin_amdgcn_mfma_f32_32x32x16_bf16(xb, xa[i], to, 0, 0, 0);
                 }
             }
-        };
-        // Step t, of index S in the cycle, its first pieces in registers: stage t + 1 is there;
-        // refill the place of stage t - 1, read the second pieces, multiply the first, read stage
-        // t + 1's first, multiply the second.
-        auto step = [&](int t, auto S) {
-            constexpr int s = decltype(S)::value, grp = (s >> 3) & 1;
-            wait_loads<(T::STAGES - 3) * T::LPW>();
-            __builtin_amdgcn_s_barrier();
-            if constexpr ((s & 7) == 0) load_scales((t >> 3) + 1, std::integral_constant<int, grp ^ 1>());
-            issue(t + T::STAGES - 1, (s + T::STAGES - 1) % T::STAGES);
-            if constexpr ((s & 1) == 0) {
-#pragma unroll
-                for (int i = 0; i < T::FM; ++i) va[i] = mx_value((uint32_t)sa[grp][i] >> (4 * (s & 7)) & 255u);
-#pragma unroll
-                for (int j = 0; j < T::FN; ++j) vb[j] = mx_value((uint32_t)sb[grp][j] >> (4 * (s & 7)) & 255u);
-            }
-            read_piece(std::integral_constant<int, s % T::STAGES>(), std::integral_constant<int, 1>());
-            multiply(std::integral_constant<int, 0>());
-            read_piece(std::integral_constant<int, (s + 1) % T::STAGES>(), std::integral_constant<int, 0>());
-            multiply(std::integral_constant<int, 1>());
-        };
-        if (n > 0) {
-            load_scales(0, std::integral_constant<int, 0>());
-#pragma unroll
-            for (int i = 0; i < T::STAGES - 1; ++i) issue(i, i);
-            wait_loads<(T::STAGES - 2) * T::LPW>();
-            __builtin_amdgcn_s_barrier();
-            read_piece(std::integral_constant<int, 0>(), std::integral_constant<int, 0>());
-            for (int t = 0; t < n; t += T::kCycle)
-                unrolled_steps<T::kCycle>([&](auto S) {
-                    constexpr int s = decltype(S)::value;
-                    if (t + s >= n) return false;
-                    step(t + s, S);
-                    return true;
-                });
         }
+    };
+    // A whole stage's operands in registers ahead: step t, of index S in its unit and in place
+    // `stg`, has stage t + 1 there; refills its own place (its operands were read in the step
+    // before), reads stage t + 1's, multiplies its own.
+    auto step_fast = [&](int t, int stg, auto S) {
+        constexpr int s = decltype(S)::value, buf = s & 1;
+        wait_loads<(T::STAGES - 2) * T::LPW>();
+        __builtin_amdgcn_s_barrier();
+        if constexpr (s == 0) {
+            next_unit();
+            load_scales((t >> 3) + 1);
+        }
+        issue(t + T::STAGES, stg);
+        read_stage(stg + 1 == T::STAGES ? 0 : stg + 1, std::integral_constant<int, buf ^ 1>());
+        multiply_stage(S, std::integral_constant<int, buf>());
+        constexpr int kReads = 2 * (T::FM + T::FN), kMfma = T::FM * T::FN, kPer = (kReads + kMfma - 1) / kMfma;
+#pragma unroll
+        for (int g = 0; g < kMfma; ++g) {
+            __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);          // an MFMA
+            __builtin_amdgcn_sched_group_barrier(0x100, kPer, 0);       // LDS reads
+        }
+    };
+    // In bf16 a stage's two pieces one by one, the first in registers: stage t + 1 is there;
+    // refill the place of stage t - 1, read the second piece, multiply the first, read stage
+    // t + 1's first, multiply the second.
+    auto step_exact = [&](int t, int stg, auto S) {
+        constexpr int s = decltype(S)::value;
+        typedef std::integral_constant<int, 0> First;
+        typedef std::integral_constant<int, 1> Second;
+        wait_loads<(T::STAGES - 3) * T::LPW>();
+        __builtin_amdgcn_s_barrier();
+        if constexpr (s == 0) {
+            next_unit();
+            load_scales((t >> 3) + 1);
+        }
+        issue(t + T::STAGES - 1, stg == 0 ? T::STAGES - 1 : stg - 1);
+        if constexpr ((s & 1) == 0) {
+#pragma unroll
+            for (int i = 0; i < T::FM; ++i) va[i] = mx_value((uint32_t)sa[i] >> (4 * s) & 255u);
+#pragma unroll
+            for (int j = 0; j < T::FN; ++j) vb[j] = mx_value((uint32_t)sb[j] >> (4 * s) & 255u);
+        }
+        read_piece(stg, Second());
+        multiply_piece(First());
+        read_piece(stg + 1 == T::STAGES ? 0 : stg + 1, First());
+        multiply_piece(Second());
+    };
+    if (n > 0) {
+        constexpr int kFirst = EXACT ? T::STAGES - 1 : T::STAGES;
+        load_scales(0);
+#pragma unroll
+        for (int i = 0; i < kFirst; ++i) issue(i, i);
+        wait_loads<(kFirst - 1) * T::LPW>();
+        __builtin_amdgcn_s_barrier();
+        typedef std::integral_constant<int, 0> First;
+        if constexpr (EXACT) read_piece(0, First());
+        else read_stage(0, First());
+        int place = 0;
+        for (int t = 0; t < n; t += T::kCycle)
+            unrolled_steps<T::kCycle>([&](auto S) {
+                constexpr int s = decltype(S)::value;
+                if (t + s >= n) return false;
+                const int stg = T::kCycle % T::STAGES == 0 ? s % T::STAGES : place;     // known where the ring fits a unit
+                if constexpr (EXACT) step_exact(t + s, stg, S);
+                else step_fast(t + s, stg, S);
+                place = place + 1 == T::STAGES ? 0 : place + 1;
+                return true;
+            });
+    }
+    if constexpr (TWO) {
+#pragma unroll
+        for (int e = 0; e < 16; ++e) acc[0][0][e] += other[e];
     }
 
     // ---- epilogue: kCols columns of a wave's 32 rows at a time through LDS, out in whole lines ----
@@ -413,14 +431,22 @@ __global__ __launch_bounds__(T::kThreads, T::kOccupancy) void k_f8_gemm_pair(F8P
 #endif
 }
 
-// Sum of the split-K partials, in the order of the splits.
+// Sum of the split-K partials, in the order of the splits, four columns a thread.
 __global__ __launch_bounds__(256) void k_f8_reduce(const float* part, int splits, int64_t M, int64_t N, void* C, int type, int64_t ldc) {
-    const int64_t n = M * N;
-    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (int64_t)gridDim.x * 256) {
-        float s = 0.0f;
-        for (int k = 0; k < splits; ++k) s += part[k * n + i];
-        const int64_t r = i / N;
-        store_out(C, type, r * ldc + (i - r * N), s);
+    const int64_t n = M * N, per = (N + 3) / 4;
+    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < M * per; i += (int64_t)gridDim.x * 256) {
+        const int64_t r = i / per, c = (i - r * per) * 4;
+        const float* src = part + r * N + c;
+        v4f s = {0.0f, 0.0f, 0.0f, 0.0f};
+        if (c + 4 <= N) {
+            for (int k = 0; k < splits; ++k) s += *reinterpret_cast<const f32x4_any*>(src + k * n);
+        } else {
+            for (int k = 0; k < splits; ++k)
+                for (int e = 0; e < 4 && c + e < N; ++e) s[e] += src[k * n + e];
+        }
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            if (c + e < N) store_out(C, type, r * ldc + c + e, s[e]);
     }
 }
 
@@ -587,7 +613,7 @@ enum F8TileKind { kWide, kMid, kSmall };
 // Tiles by the size of the product.
 F8TileKind tile_kind(const F8GemmArgs& a) {
     const auto tiles = [&](int64_t m, int64_t n) { return ((a.M + m - 1) / m) * ((a.N + n - 1) / n); };
-    if (tiles(256, 256) >= 192) return kWide;
+    if (tiles(128, 256) >= 400) return kWide;
     return tiles(128, 128) >= 240 ? kMid : kSmall;
 }
 
@@ -595,7 +621,7 @@ template <class T>
 F8Product product_of(const F8GemmArgs& a) {
     F8Product d{};
     d.a = a;
-    d.splits = (int)f8_gemm_splits(a.M, a.N, a.K);
+    d.splits = (int)f8_gemm_splits(a.M, a.N, a.K, a.type);
     d.tiles_n = (uint32_t)((a.N + T::BN - 1) / T::BN);
     d.tiles_m = (uint32_t)((a.M + T::BM - 1) / T::BM);
     d.blocks = d.tiles_m * d.tiles_n * (uint32_t)d.splits;
@@ -605,7 +631,7 @@ F8Product product_of(const F8GemmArgs& a) {
 hipError_t reduce(const F8Product& d, hipStream_t s) {
     if (d.splits == 1) return hipSuccess;
     const F8GemmArgs& a = d.a;
-    k_f8_reduce<<<(uint32_t)std::min<int64_t>((a.M * a.N + 255) / 256, 4096), 256, 0, s>>>(a.part, d.splits, a.M, a.N, a.C, a.type, a.ldc);
+    k_f8_reduce<<<(uint32_t)std::min<int64_t>((a.M * ((a.N + 3) / 4) + 255) / 256, 4096), 256, 0, s>>>(a.part, d.splits, a.M, a.N, a.C, a.type, a.ldc);
     return hipGetLastError();
 }
 
@@ -624,8 +650,7 @@ hipError_t pair(const F8GemmArgs& a, const F8GemmArgs& b, hipStream_t s) {
     const uint32_t blocks = (uint32_t)round_up(da.blocks, 8) + db.blocks;
     if (a.type == SQ_TYPE_F32 && b.type == SQ_TYPE_F32) k_f8_gemm_pair<T, true, true><<<blocks, T::kThreads, 0, s>>>(da, db);
     else if (a.type == SQ_TYPE_F32) k_f8_gemm_pair<T, true, false><<<blocks, T::kThreads, 0, s>>>(da, db);
-    else if (b.type == SQ_TYPE_F32) k_f8_gemm_pair<T, false, true><<<blocks, T::kThreads, 0, s>>>(da, db);
-    else k_f8_gemm_pair<T, false, false><<<blocks, T::kThreads, 0, s>>>(da, db);
+    else k_f8_gemm_pair<T, false, true><<<blocks, T::kThreads, 0, s>>>(da, db);
     hipError_t e = hipGetLastError();
     if (e == hipSuccess) e = reduce(da, s);
     return e == hipSuccess ? reduce(db, s) : e;
@@ -642,10 +667,11 @@ hipError_t rows(const F8RowsArgs& a, hipStream_t s) {
 
 }  // namespace
 
-// Few tiles of a long inner axis are split, in parts of at least 20 tiles.
-int64_t f8_gemm_splits(int64_t M, int64_t N, int64_t K) {
-    const int64_t tiles = ((M + 63) / 64) * ((N + 63) / 64), k = (K + kMxTile - 1) / kMxTile;
-    return std::max<int64_t>(1, std::min<int64_t>(512 / std::max<int64_t>(tiles, 1), k / 20));
+// Few tiles of a long inner axis are split, in parts of at least 20 tiles (16 where
+// these take the slower instruction).
+int64_t f8_gemm_splits(int64_t M, int64_t N, int64_t K, int type) {
+    const int64_t tiles = ((M + 63) / 64) * ((N + 63) / 64), k = (K + kMxTile - 1) / kMxTile, least = type == SQ_TYPE_F32 ? kSplitExact : kSplit;
+    return std::max<int64_t>(1, std::min<int64_t>(512 / std::max<int64_t>(tiles, 1), k / least));
 }
 
 hipError_t launch_f8_gemm(const F8GemmArgs& a, hipStream_t s) {
@@ -658,7 +684,7 @@ hipError_t launch_f8_gemm(const F8GemmArgs& a, hipStream_t s) {
 }
 
 hipError_t launch_f8_gemm_pair(const F8GemmArgs& a, const F8GemmArgs& b, hipStream_t s) {
-    if (a.M == 0 || a.N == 0 || b.M == 0 || b.N == 0 || tile_kind(a) != tile_kind(b)) {
+    if (a.M == 0 || a.N == 0 || b.M == 0 || b.N == 0 || tile_kind(a) != tile_kind(b) || (a.type != SQ_TYPE_F32 && b.type != SQ_TYPE_F32)) {
         const hipError_t e = launch_f8_gemm(a, s);
         return e == hipSuccess ? launch_f8_gemm(b, s) : e;
     }
