@@ -452,13 +452,11 @@ __global__ __launch_bounds__(256) void k_f8_reduce(const float* part, int splits
 
 // ---------------------------------------------------------------------------
 // Few rows of values: Y = X W^T, bound by the one read of W.  A wave loads 16 x 128
-// tiles of W straight into registers; a block owns 16 rows and 16 columns, its
-// eight waves share the inner axis in contiguous parts.  Four lanes hold the 128
+// tiles of W straight into registers; a block owns 16 rows and 16 FN columns, its
+// waves share the inner axis in contiguous parts, U tiles in flight each.  Four lanes hold the 128
 // elements of X of a row and tile and quantize them in registers.  The waves' sums
 // meet in LDS in a fixed order.
 // ---------------------------------------------------------------------------
-constexpr int kRowsWaves = 8;
-
 // Codes of 32 values in the words w (bf16 pairs, or fp32), with the block's scale byte.
 template <bool BF16>
 __device__ __forceinline__ v8i quantize_lane(const uint32_t* w, int& scale_byte) {
@@ -496,7 +494,7 @@ __device__ __forceinline__ v8i quantize_lane(const uint32_t* w, int& scale_byte)
     return a;
 }
 
-template <typename T, int FN, int U, bool EXACT>
+template <typename T, int FN, int U, int kRowsWaves, bool EXACT>
 __global__ __launch_bounds__(64 * kRowsWaves, 4) void k_f8_rows(F8RowsArgs p, uint32_t tiles_n) {
 #if defined(__HIP_DEVICE_COMPILE__)
     constexpr int kLd = 16 * FN + 4, kWords = 32 * sizeof(T) / 4, kHalf = kWords / 2, kV = 16 / sizeof(T);
@@ -656,12 +654,12 @@ hipError_t pair(const F8GemmArgs& a, const F8GemmArgs& b, hipStream_t s) {
     return e == hipSuccess ? reduce(db, s) : e;
 }
 
-template <typename T, int FN, int U>
+template <typename T, int FN, int U, int WAVES>
 hipError_t rows(const F8RowsArgs& a, hipStream_t s) {
     const int64_t tiles_n = (a.N + 16 * FN - 1) / (16 * FN);
     const uint32_t blocks = (uint32_t)((a.M + 15) / 16 * tiles_n);
-    if (a.out_type == SQ_TYPE_F32) k_f8_rows<T, FN, U, true><<<blocks, 64 * kRowsWaves, 0, s>>>(a, (uint32_t)tiles_n);
-    else k_f8_rows<T, FN, U, false><<<blocks, 64 * kRowsWaves, 0, s>>>(a, (uint32_t)tiles_n);
+    if (a.out_type == SQ_TYPE_F32) k_f8_rows<T, FN, U, WAVES, true><<<blocks, 64 * WAVES, 0, s>>>(a, (uint32_t)tiles_n);
+    else k_f8_rows<T, FN, U, WAVES, false><<<blocks, 64 * WAVES, 0, s>>>(a, (uint32_t)tiles_n);
     return hipGetLastError();
 }
 
@@ -706,9 +704,17 @@ bool f8_rows_ok(int64_t M, int64_t K, int64_t N, int type) {
 
 hipError_t launch_f8_rows(const F8RowsArgs& a, hipStream_t s) {
     if (a.M == 0 || a.N == 0) return hipSuccess;
-    const bool many = ((a.M + 15) / 16) * ((a.N + 15) / 16) >= 512;
-    if (a.type == SQ_TYPE_F32) return many ? rows<float, 2, 1>(a, s) : rows<float, 1, 1>(a, s);
-    return many ? rows<uint16_t, 2, 2>(a, s) : rows<uint16_t, 1, 2>(a, s);
+    // One tile of rows: as many blocks as there are (1 x 4096 -> 11008 in bf16 11.6 us, with 32 columns a block 12.3), fp32
+    // rows with twice the waves where these have two tiles each (1 x 4096 -> 4096 6.8 us, 7.9 with eight).  More rows:
+    // columns that share the rows' codes (64 x 4096 -> 4096 10.5 us with 64 columns a block, 12.8 with 32, 19.6 with 16;
+    // 128 x 1024 -> 1024, 512 tiles, 3.9 with 32 and 4.2 with 64).
+    const int64_t tiles_m = (a.M + 15) / 16, tiles = tiles_m * ((a.N + 15) / 16);
+    if (tiles_m > 1 && tiles >= 512) {
+        if (a.type == SQ_TYPE_F32) return tiles >= 1024 ? rows<float, 4, 1, 8>(a, s) : rows<float, 2, 1, 8>(a, s);
+        return tiles >= 1024 ? rows<uint16_t, 4, 1, 8>(a, s) : rows<uint16_t, 2, 1, 8>(a, s);
+    }
+    if (a.type == SQ_TYPE_F32) return a.K >= 32 * kMxTile ? rows<float, 1, 1, 16>(a, s) : rows<float, 1, 1, 8>(a, s);
+    return rows<uint16_t, 1, 2, 8>(a, s);
 }
 
 }  // namespace sq
