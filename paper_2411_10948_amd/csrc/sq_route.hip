@@ -330,12 +330,14 @@ __global__ __launch_bounds__(1024) void k_route_lanes(RouteArgs p, int lanes, in
     load_run<T, R>(row, min(e0, p.E - 1), n, p.E, none, l);
     bool bad = false;
     float m = none;
+    if (softmax || !EXACT) {
 #pragma unroll
-    for (int r = 0; r < R; ++r) {
-        bad |= l[r] != l[r] || (softmax && l[r] == __builtin_inff());
-        m = fmaxf(m, l[r]);
+        for (int r = 0; r < R; ++r) {
+            if constexpr (!EXACT) bad |= l[r] != l[r] || (softmax && l[r] == __builtin_inff());
+            m = fmaxf(m, l[r]);
+        }
+        m = max16(m);
     }
-    m = max16(m);
     float sum = 1.0f;
     if (softmax && (EXACT || !p.renorm)) {
         float part[4] = {0.0f, 0.0f, 0.0f, 0.0f};
@@ -347,24 +349,31 @@ __global__ __launch_bounds__(1024) void k_route_lanes(RouteArgs p, int lanes, in
     uint32_t key[R];
     float doubt = 0.0f;     // how far fp32 may be off the difference of two sums s + bias, without its rounding
     if constexpr (EXACT) {
-        float bias[R], inv = 1.0f / sum, a = none, b = none, peak = 0.0f;
+        float bias[R], inv = 1.0f / sum, a = none, b = none;
+#pragma unroll
+        for (int r = 0; r < R; ++r) bias[r] = 0.0f;
         if (p.bias) load_run<float, R>(p.bias, min(e0, p.E - 1), n, p.E, 0.0f, bias);
 #pragma unroll
         for (int r = 0; r < R; ++r) {
             const float s = softmax ? __expf(l[r] - m) * inv : __builtin_amdgcn_rcpf(1.0f + __expf(-l[r]));
-            const float v = l[r] > none ? (p.bias ? s + bias[r] : s) : none;
-            peak = fmaxf(peak, l[r] > none ? s : 0.0f);
+            // NaN in the logit or the bias, and +inf under softmax (inf - inf), are NaN here
+            const float v = l[r] == none ? none : s + bias[r];
             bad |= v != v;
-            b = larger(b, v < a ? v : a);
-            a = larger(a, v);
-            // a sum with a bias is in doubt anyway: its last bits say which of the lane's it is
-            key[r] = !p.bias ? ordered(l[r]) : v > none ? (ordered(v) & ~(uint32_t)(R - 1)) | (uint32_t)(R - 1 - r) : 0u;
+            b = __builtin_amdgcn_fmed3f(a, b, v);       // the second of three, as b <= a
+            a = fmaxf(a, v);
+            if (p.bias) {
+                // a sum with a bias is in doubt anyway: its last bits say which of the lane's it is
+                const uint32_t u = __float_as_uint(v), o = u ^ ((uint32_t)((int32_t)u >> 31) | 0x80000000u);
+                key[r] = v == none ? 0u : (o & ~(uint32_t)(R - 1)) | (uint32_t)(R - 1 - r);
+            } else {
+                key[r] = ordered(l[r]);
+            }
         }
         // exp(x): the rounding of x log2(e) moves a score by at most s |x| 2^-24 or, a sigmoid, s (1 - s) |x| 2^-24, less
         // than half of 2^-24 of the largest; the exponential and the reciprocal are good to 1 ulp, sums are rounded once.
         // So two sigmoids' difference is right to 2^-21; a softmax's sum of at most 14 additions one after the other is a
         // factor of all scores, which moves differences by 20 2^-24 of the largest at most.
-        doubt = max16(peak) * (softmax ? 0x1p-18f : 0x1p-21f);
+        doubt = softmax ? inv * 0x1p-18f : 0x1p-21f;     // the largest softmax is 1 / sum
         if (p.groups > 1) {
             for (int step = 1; step < lanes; step <<= 1) {
                 const float oa = step == 1 ? row_move<kLane1>(a) : step == 2 ? row_move<kLane2>(a) : row_move<kMirror8>(a);
@@ -380,8 +389,10 @@ __global__ __launch_bounds__(1024) void k_route_lanes(RouteArgs p, int lanes, in
             }
             const bool mine = g < p.groups, kept = mine && rank < p.top_groups;
             const float low = -max16(kept ? -total : none), high = max16(mine && !kept ? total : none);
-            // of equal totals the lowest group, but only fp64 knows which are equal
-            if (high > none && !(low - high > 2.0f * doubt + 0x1p-20f * (fabsf(low) + fabsf(high)))) bad = true;
+            // Of equal totals the lowest group, but only fp64 knows which are equal: two sums with a bias and their total
+            // are rounded, 3 2^-24 of the summands' size, on either side.
+            const float size = max16(mine && a > none ? fabsf(a) + (b > none ? fabsf(b) : 0.0f) : 0.0f);
+            if (high > none && !(low - high > 2.0f * doubt + 0x1p-21f * size)) bad = true;
 #pragma unroll
             for (int r = 0; r < R; ++r) key[r] = kept ? key[r] : 0u;
         }
