@@ -28,7 +28,7 @@ hipError_t launch_norm_backward(const NormArgs& a, hipStream_t s);   // x is the
 
 // ---- router (sq_route.hip) ----
 constexpr int kRouteMaxExperts = 1024, kRouteMaxTopK = 64, kRouteMaxGroups = 64;
-constexpr int64_t kRouteMaxTokens = (int64_t)1 << 26;     // 2^32 threads a launch
+constexpr int64_t kRouteMaxTokens = ((int64_t)1 << 26) - 4;     // at most: four a block of 256 threads, below 2^32 threads
 constexpr int kRouteTokens = 64;        // of a block: a bit each in a word by expert
 struct RouteArgs {
     int type, score, renorm;            // SQ_TYPE_*, SQ_SCORE_*

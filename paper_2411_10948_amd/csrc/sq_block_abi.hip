@@ -27,7 +27,7 @@ sq_status check_stats(const float* stats) {
 
 sq_status check_route_tokens(int64_t T) {
     SQ_TRY(check_dim(T, kMaxRows, "T"));
-    if (T >= kRouteMaxTokens) return fail(SQ_ERR_UNSUPPORTED, "2^26 tokens or more");
+    if (T > kRouteMaxTokens) return fail(SQ_ERR_UNSUPPORTED, "more than 2^26 - 4 tokens");
     return SQ_OK;
 }
 

@@ -82,6 +82,8 @@ def test_router(L):
     assert _size(L.sq_route_workspace_size, 64, 64) == (0, 0)       # one launch
     assert _size(L.sq_route_workspace_size, 64, 0)[0] == _size(L.sq_route_workspace_size, 64, 1025)[0] == INVALID
     assert _size(L.sq_route_workspace_size, 1 << 26, 64)[0] == UNSUPPORTED
+    assert _size(L.sq_route_workspace_size, (1 << 26) - 3, 64)[0] == UNSUPPORTED       # a launch of 2^32 threads
+    assert _size(L.sq_route_workspace_size, (1 << 26) - 4, 64)[0] == 0
 
     names = "d l type T E ld score k renorm scale share chosen dl ld_d stream".split()
     ok = [P, P, 0, 100, 64, 64, 0, 8, 0, 1.0, P, P, P, 64, None]
