@@ -915,7 +915,7 @@ sq_status sq_norm_backward(const void* dY, const void* H, const void* dH, int32_
  *   offsets [E + 1] rows of expert e: [offsets[e], offsets[e + 1])
  * A token with NaN among its logits (or s + bias), or +Inf under softmax, has
  * chosen = place = -1 and share NaN.
- * Sizes: T < 2^26, T k < 2^31, E <= 1024, k <= 64, groups <= 64 (SQ_ERR_UNSUPPORTED).
+ * Sizes: T <= 2^26 - 4, T k < 2^31, E <= 1024, k <= 64, groups <= 64 (SQ_ERR_UNSUPPORTED).
  * Workspace: sq_route_workspace_size bytes (0: none), 16-byte aligned.
  *
  * sq_route_backward -- the logits' gradient from dshare [T, k], the forward's
@@ -977,7 +977,9 @@ sq_status sq_exchange_combine_backward(const void* dout, const void* R, int32_t 
  *   a block that holds NaN or Inf: s = 255, which stands for NaN in all of it.
  * Values that a code and scale stand for are exact in bf16 and fp32, but those
  * past their range (of a block with a > 1.8125 * 2^127: Inf) and, of scales below
- * 2^-117 (bf16) or 2^-140, those below their subnormals' step.
+ * 2^-124 (bf16) or 2^-140 (fp32), those off their least step (2^-133, 2^-149).
+ * Products with an fp32 result take the values in bf16, sums in fp32 (24 bits kept);
+ * with a bf16 result sums of 16 products first, each cut 13 bits below the largest.
  *
  * Layout of a matrix [rows, K] (sq_f8_size bytes): rows in groups of 16, K in units
  * of 512.  Element (r, k) is byte

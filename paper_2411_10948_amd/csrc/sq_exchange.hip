@@ -6,8 +6,10 @@
 //                      dshare[t, j] = <dout[t], rows[place[t, j]]>
 //   dispatch's         dx[t] = sum_j drows[place[t, j]] (+ add[t]): combine without shares
 // A place outside [0, rows) is no row: nothing is read or written for it, its
-// product is 0.  Each row is read or written once; bound by HBM, small calls by
-// their one launch.
+// product is 0.  Each row is read or written once, 16 bytes a thread, a thread's next
+// slots' rows on their way while it adds up or multiplies; bound by HBM, small calls by
+// their one launch.  4096 tokens, 8 rows of 2048 each in bf16 (134 MB of rows): dispatch
+// 27 us, combine 29, its gradient 53, dispatch's 30: 738 MB at 5.3 TB/s in all.
 #include <algorithm>
 #include <type_traits>
 
@@ -152,9 +154,13 @@ dim3 grid_of(int64_t T_, int64_t D, int& tpr) {
     return dim3((uint32_t)std::min<int64_t>((T_ + kThreads / tpr - 1) / (kThreads / tpr), kMaxGrid), (uint32_t)((n + tpr - 1) / tpr));
 }
 
-// f(slots in flight, whether the rows go past the caches) as compile-time constants
+// f(slots in flight, whether the rows go past the caches) as compile-time constants.  No
+// more slots than there are: combine's gradient of 1187 x 1000 in fp32 with two 5.3 us,
+// with room for eight 8.1; with four 8.8 and 12.5.
 template <typename T, class F>
 hipError_t with_rows(const ExchangeArgs& a, F f) {
+    // Rows that the last-level cache would not keep anyway go past it: 134 MB, combine and dispatch's gradient 29 and 30 us
+    // instead of 37 and 47, the two that write rows the same either way.  Smaller ones stay for the kernel that reads them next.
     const bool nt = (double)a.T * a.k * (double)a.D * sizeof(T) >= 32e6;
     const auto slots = [&](auto NT) {
         if (a.k <= 2) return f(std::integral_constant<int, 2>(), NT);

@@ -13,7 +13,10 @@
 // 6.5e-5 where channels differ in size: nothing next to the 2^-9 of a result in
 // bf16, but too much for one in fp32.  Those (EXACT) take the codes' values in bf16,
 // which holds code and scale together, and v_mfma_f32_32x32x16_bf16, whose sums keep
-// 24 bits: 1e-8 to 1e-7, at 1.7 instead of 4.6 PFLOP/s (register loops on random codes).
+// 24 bits: 1e-8 to 1e-7, at 1.8 instead of 4.0 PFLOP/s (register loops on random codes).
+// Bound by the power that the matrix instructions take: 4096 x 11008 x 8192 runs at 2.5
+// PFLOP/s with bf16 results and at 1.37 with fp32 (a bf16 library product of 8192^3 at
+// 1.25), small ones by the launch and the first loads.
 #include <algorithm>
 #include <type_traits>
 
@@ -608,7 +611,11 @@ __global__ __launch_bounds__(64 * kRowsWaves, 4) void k_f8_rows(F8RowsArgs p, ui
 
 enum F8TileKind { kWide, kMid, kSmall };
 
-// Tiles by the size of the product.
+// Tiles by the size of the product.  us in bf16 / fp32:
+//   128 x 256 and 128 x 128: 4096^3 (512 large tiles) 58 / 107 and 62 / 117, 8192 x 8192 x 512 48 / 76 and 55 / 85,
+//     3000^3 (288) 38 / 67 and 34 / 63;
+//   128 x 128 and 64 x 64: 2048^3 (256) 10.7 / 20.9 and 14.1 / 21.5, 1024 x 4096 x 1024 (256) 7.8 / 13.4 and 9.5 / 12.9,
+//     1500^3 (144) 9.6 / 16.2 and 9.7 / 14.0, 512 x 4096 x 4096 (128) 16 / 33 and 14 / 24.
 F8TileKind tile_kind(const F8GemmArgs& a) {
     const auto tiles = [&](int64_t m, int64_t n) { return ((a.M + m - 1) / m) * ((a.N + n - 1) / n); };
     if (tiles(128, 256) >= 400) return kWide;
@@ -666,7 +673,9 @@ hipError_t rows(const F8RowsArgs& a, hipStream_t s) {
 }  // namespace
 
 // Few tiles of a long inner axis are split, in parts of at least 20 tiles (16 where
-// these take the slower instruction).
+// these take the slower instruction): the sum of the parts is a launch more, 5 to 6 us.
+// fp32 results: 300 x 300 x 8192 (64 tiles) whole 29 us, in parts of 20 16.9, of 16
+// 13.4; 768 x 768 x 3152 (25) whole 14, in halves 15.8; 1024^3 (8) 7.0 and 13.9.
 int64_t f8_gemm_splits(int64_t M, int64_t N, int64_t K, int type) {
     const int64_t tiles = ((M + 63) / 64) * ((N + 63) / 64), k = (K + kMxTile - 1) / kMxTile, least = type == SQ_TYPE_F32 ? kSplitExact : kSplit;
     return std::max<int64_t>(1, std::min<int64_t>(512 / std::max<int64_t>(tiles, 1), k / least));
@@ -696,7 +705,10 @@ hipError_t launch_f8_gemm_pair(const F8GemmArgs& a, const F8GemmArgs& b, hipStre
     }
 }
 
-// Few rows, for which the products' tiles would be mostly empty.
+// Few rows, for which the products' tiles would be mostly empty.  bf16, and the quantizer
+// with the product: 64 x 4096 -> 4096 (38912 of the 40000) 9.2 us, 13.5; 96 rows of it
+// (58368) 14.4, 14.0; 512 x 1024 -> 1024 (28672) 6.1, 8.7; fp32: 512 x 768 -> 768
+// (36864) 7.1, 9.5, 32 x 4096 -> 4096 (38912) 11.3, 15.5.
 bool f8_rows_ok(int64_t M, int64_t K, int64_t N, int type) {
     const double blocks = (double)((M + 15) / 16) * (double)((N + 15) / 16), steps = (double)((K + 127) / 128);
     return M <= 16 || blocks * (steps + 6.0) * (type == SQ_TYPE_F32 ? 2.0 : 1.0) <= 40000.0;

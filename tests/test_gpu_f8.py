@@ -207,6 +207,28 @@ def test_products_are_exact_where_sums_are(f8, M, N, K):
     assert (C.double() == want).all()
 
 
+# where the codes' values pass below the normal numbers of fp32 and bf16
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("e", [-105, -116, -122, -140])
+@pytest.mark.parametrize("M,N,K", [(5, 40, 700), (150, 270, 1400)])
+def test_products_of_tiny_values(f8, M, N, K, e, dtype):
+    import torch
+    rng = np.random.default_rng(M)
+    x, w = _cuda(np.ldexp(rng.standard_normal((M, K)), e), "f32"), _cuda(np.ldexp(rng.standard_normal((N, K)), 100), "f32")
+    a, b = f8.quantize(x)[0], f8.quantize(w, True)[0]
+    va, vb = ref.f8_values(_np(x)), ref.f8_values(_np(w), True)
+    want, y = va @ vb.T, torch.empty(M, N, dtype=_dtype(dtype), device="cuda")
+    need = f8.sq_f8_linear_workspace_size(M, K, N)
+    f8.sq_f8_linear(x, b.codes, b.scales, y, torch.empty(need, dtype=torch.uint8, device="cuda") if need else None)
+    tol = (np.abs(va) @ np.abs(vb).T) * (K + 2) * 2.0 ** -23
+    if dtype == "bf16":
+        tol = tol + 15 * 2.0 ** -13 * (_pieces(va) @ _pieces(vb).T) + 2.0 ** -8 * np.abs(want)
+    else:       # operands in bf16, whose least step is 2^-133
+        tol = tol + 2.0 ** -134 * np.abs(vb).sum(1)
+    np.testing.assert_array_less(np.abs(_np(y) - want), tol + 2.0 ** -149)
+    np.testing.assert_array_equal(a.values().double().cpu().numpy(), np.round(va * 2.0 ** 149) / 2.0 ** 149)
+
+
 def test_scales_reach_every_block(f8):
     # each block of 128 with a scale of its own on both sides
     import torch
