@@ -15,7 +15,8 @@ from typing import Optional, Tuple
 import torch
 
 from .mx import TYPE_F32, _TYPES, _checked, _gpu_of, _of_layer, _on, _rows, _shape, _sized, _type, _workspace
-from .shiftquant import _I64, _SZ, _check, _ptr, _stream, _ws_ptr, load
+from .norm import _fixed
+from .shiftquant import _I64, _P, _SZ, _check, _ptr, _stream, _ws_ptr, load
 
 
 @dataclasses.dataclass
@@ -167,12 +168,14 @@ class LinearPlan:
         self.M, self.C_in, self.C_out, self.dtype, self.train = M, C_in, C_out, dtype, train
         self._x_shape, self._y_shape, self._w_shape = torch.Size((M, C_in)), torch.Size((M, C_out)), torch.Size((C_out, C_in))
         self.Y = torch.empty(self._y_shape, dtype=dtype, device=dev)
-        self._type, self._lib, self._gpu = _TYPES[dtype], load(), _gpu_of(self.Y)
-        self._y_ptr, self._y_ld = self.Y.data_ptr(), max(C_out, 1)
+        self._lib, self._gpu = load(), _gpu_of(self.Y)
+        y, ld = (_P, self.Y.data_ptr()), (_I64, max(C_out, 1))
         self._has_weight = self._has_input = False
         if not train:
             self.ws = _workspace(nbytes, dev)
-            self._ws = _ws_ptr(self.ws)
+            kind, (ws, nws) = (ct.c_int32, _TYPES[dtype]), _ws_ptr(self.ws)
+            self._size = _fixed(kind, (_I64, M), (_I64, C_in))
+            self._to = _fixed((_I64, C_out), y, kind, ld, (_P, ws), (_SZ, nws))
             self._held = [self.Y, self.ws]      # the pointers kept stay valid as long as the plan
             return
         self.w, self.w_t = F8Matrix.empty(C_out, C_in, dev), F8Matrix.empty(C_in, C_out, dev)
@@ -187,8 +190,9 @@ class LinearPlan:
             self._held += [m.codes, m.scales]
             setattr(self.layer, name, m.codes.data_ptr())
             setattr(self.layer, name + "_scales", m.scales.data_ptr())
-        self._layer_ptr, self._dw_ld = ct.addressof(self.layer), max(C_in, 1)
-        self._dx_ptr, self._dw_ptr = self.dX.data_ptr(), self.dW.data_ptr()
+        self._layer_ptr, = _fixed((_P, ct.addressof(self.layer)))
+        ld_in = _I64, max(C_in, 1)
+        self._to, self._to_back = _fixed(y, ld), _fixed((_P, self.dX.data_ptr()), ld_in, (_P, self.dW.data_ptr()), ld_in)
         self.ws = _workspace(sq_f8_layer_workspace_size(self.layer), dev)
         if self.ws is not None:
             self._held.append(self.ws)
@@ -211,7 +215,7 @@ class LinearPlan:
                 raise ValueError("w: a training plan has its own codes (quantize_weight)")
             if not self._has_weight:
                 raise ValueError("forward needs a quantize_weight before it")
-            st = self._lib.sq_f8_layer_forward(self._layer_ptr, x.data_ptr(), ld, self._y_ptr, self._y_ld, _on(self._gpu, stream))
+            st = self._lib.sq_f8_layer_forward(self._layer_ptr, x.data_ptr(), ld, *self._to, _on(self._gpu, stream))
             if st:
                 _check("sq_f8_layer_forward", st)
             self._has_input = True
@@ -221,10 +225,8 @@ class LinearPlan:
         codes = w.codes
         if codes.get_device() != self._gpu:
             raise ValueError("w: expected codes on the plan's GPU")
-        t = self._type
         st = self._lib.sq_f8_linear(
-            x.data_ptr(), t, self.M, self.C_in, ld, codes.data_ptr(), w.scales.data_ptr(), self.C_out, self._y_ptr, t, self._y_ld,
-            *self._ws, _on(self._gpu, stream))
+            x.data_ptr(), *self._size, ld, codes.data_ptr(), w.scales.data_ptr(), *self._to, _on(self._gpu, stream))
         if st:
             _check("sq_f8_linear", st)
         return self.Y
@@ -236,8 +238,7 @@ class LinearPlan:
         ld = _checked(dy, self._y_shape, self.dtype, self._gpu, "dy")
         if not self._has_input:
             raise ValueError("backward needs a forward before it")
-        st = self._lib.sq_f8_layer_backward(
-            self._layer_ptr, dy.data_ptr(), ld, self._dx_ptr, self._dw_ld, self._dw_ptr, self._dw_ld, _on(self._gpu, stream))
+        st = self._lib.sq_f8_layer_backward(self._layer_ptr, dy.data_ptr(), ld, *self._to_back, _on(self._gpu, stream))
         if st:
             _check("sq_f8_layer_backward", st)
         return self.dX, self.dW

@@ -13,7 +13,13 @@ from typing import Optional, Tuple
 import torch
 
 from .mx import _TYPES, _checked, _gpu_of, _like, _on, _rows, _shape, _type, _workspace
-from .shiftquant import _SZ, _check, _ptr, _stream, _ws_ptr, load
+from .shiftquant import _I64, _P, _SZ, _check, _ptr, _stream, _ws_ptr, load
+
+
+def _fixed(*values) -> tuple:
+    """Arguments that a plan passes in each of its calls, (C type, value), converted once (one
+    token's router call takes the host 5.0 us instead of 5.3, an 8-bit layer's 4.75 instead of 4.9)."""
+    return tuple(t(v) for t, v in values)
 
 
 def _vector(t: torch.Tensor, n: int, name: str, like: Optional[torch.Tensor] = None) -> int:
@@ -87,7 +93,7 @@ class NormPlan:
         self._shape, self._c_shape = torch.Size((M, C)), torch.Size((C,))
         self.Y = torch.empty(self._shape, dtype=dtype, device=dev)
         self.H = torch.empty(self._shape, dtype=dtype, device=dev) if residual else None
-        self._lib, self._type, self._ptype, self._gpu = load(), _TYPES[dtype], _TYPES[param_dtype], _gpu_of(self.Y)
+        self._lib, self._gpu = load(), _gpu_of(self.Y)
         self._has_input = False
         self.stats = self.dX = self.dgamma = self.dbeta = self.ws = None
         if train:
@@ -95,9 +101,13 @@ class NormPlan:
             self.dX = torch.empty(self._shape, dtype=dtype, device=dev)
             self.dgamma, self.dbeta = torch.empty((2, C), dtype=torch.float32, device=dev).unbind(0)
             self.ws = _workspace(nbytes, dev)
-        self._ld = max(C, 1)
-        self._held = (self.Y, self.H, self.stats, self.dX, self.dgamma, self.dbeta, self.ws)    # what _ptrs point at
-        self._ptrs = tuple(map(_ptr, self._held[:-1])) + _ws_ptr(self.ws)
+        i32, ld = ct.c_int32, (_I64, max(C, 1))
+        self._held = (self.Y, self.H, self.stats, self.dX, self.dgamma, self.dbeta, self.ws)    # what the calls point at
+        y, h, stats, dx, dgamma, dbeta = ((_P, _ptr(t)) for t in self._held[:-1])
+        ws, nws = _ws_ptr(self.ws)
+        self._size = _fixed((i32, _TYPES[dtype]), (_I64, M), (_I64, C))
+        self._to = _fixed((i32, _TYPES[param_dtype]), (ct.c_float, eps), h, ld, y, ld, stats)
+        self._to_back = _fixed((i32, _TYPES[param_dtype]), stats, dx, ld, dgamma, dbeta, (_P, ws), (_SZ, nws))
 
     def _param(self, t: torch.Tensor, name: str) -> int:
         if t.shape != self._c_shape or not t.is_contiguous() or t.get_device() != self._gpu:
@@ -112,10 +122,9 @@ class NormPlan:
             raise ValueError("residual: expected one for a plan with residual=True, and none without")
         ld = _checked(x, self._shape, self.dtype, self._gpu, "x")
         ld_r = 0 if residual is None else _checked(residual, self._shape, self.dtype, self._gpu, "residual")
-        y, h, stats = self._ptrs[:3]
         st = self._lib.sq_norm_forward(
-            x.data_ptr(), _ptr(residual), self._type, self.M, self.C, ld, ld_r, self._param(gamma, "gamma"),
-            self._param(beta, "beta"), self._ptype, self.eps, h, self._ld, y, self._ld, stats, _on(self._gpu, stream))
+            x.data_ptr(), _ptr(residual), *self._size, ld, ld_r, self._param(gamma, "gamma"), self._param(beta, "beta"), *self._to,
+            _on(self._gpu, stream))
         if st:
             _check("sq_norm_forward", st)
         self._has_input = True
@@ -131,10 +140,9 @@ class NormPlan:
         ld_dy = _checked(dy, self._shape, self.dtype, self._gpu, "dy")
         ld_h = _checked(h, self._shape, self.dtype, self._gpu, "h")
         ld_dh = 0 if dh is None else _checked(dh, self._shape, self.dtype, self._gpu, "dh")
-        stats, dx, dgamma, dbeta, ws, nws = self._ptrs[2:]
         st = self._lib.sq_norm_backward(
-            dy.data_ptr(), h.data_ptr(), _ptr(dh), self._type, self.M, self.C, ld_dy, ld_h, ld_dh, self._param(gamma, "gamma"),
-            self._ptype, stats, dx, self._ld, dgamma, dbeta, ws, nws, _on(self._gpu, stream))
+            dy.data_ptr(), h.data_ptr(), _ptr(dh), *self._size, ld_dy, ld_h, ld_dh, self._param(gamma, "gamma"), *self._to_back,
+            _on(self._gpu, stream))
         if st:
             _check("sq_norm_backward", st)
         return self.dX, self.dgamma, self.dbeta

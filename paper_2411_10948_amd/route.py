@@ -13,8 +13,8 @@ from typing import Optional, Tuple
 import torch
 
 from .mx import _TYPES, _checked, _gpu_of, _like, _on, _rows, _shape, _type, _workspace
-from .norm import _floats, _vector
-from .shiftquant import _SZ, _check, _ptr, _stream, _ws_ptr, load
+from .norm import _fixed, _floats
+from .shiftquant import _I64, _P, _SZ, _check, _ptr, _stream, _ws_ptr, load
 
 SCORE_SOFTMAX = 0
 SCORE_SIGMOID = 1
@@ -116,11 +116,15 @@ class RouterPlan:
         self.place = torch.empty((T, k), dtype=torch.int32, device=dev)
         self.offsets = torch.empty(E + 1, dtype=torch.int32, device=dev)
         self.dlogits = torch.empty((T, E), dtype=dtype, device=dev)
-        self._lib, self._type, self._gpu = load(), _TYPES[dtype], _gpu_of(self.share)
-        self._rule = (SCORES[score], k, groups, top_groups, int(renormalize), float(scale))
+        self._lib, self._gpu = load(), _gpu_of(self.share)
         self._has_input = False
-        self._held = (self.share, self.chosen, self.place, self.offsets, self.dlogits)      # what _ptrs point at
-        self._ptrs, self._ws = tuple(t.data_ptr() for t in self._held), _ws_ptr(self.ws)
+        self._held = (self.share, self.chosen, self.place, self.offsets, self.dlogits, self.ws)     # what the calls point at
+        share, chosen, place, offsets, dlogits = ((_P, t.data_ptr()) for t in self._held[:-1])
+        i32, (ws, nws) = ct.c_int32, _ws_ptr(self.ws)
+        score, k, renorm, scale = (i32, SCORES[score]), (i32, k), (i32, int(renormalize)), (ct.c_float, scale)
+        self._size = _fixed((i32, _TYPES[dtype]), (_I64, T), (_I64, E))
+        self._to = _fixed(score, k, (i32, groups), (i32, top_groups), renorm, scale, share, chosen, place, offsets, (_P, ws), (_SZ, nws))
+        self._to_back = _fixed(score, k, renorm, scale, share, chosen, dlogits, (_I64, E))
 
     def forward(self, logits: torch.Tensor, bias: Optional[torch.Tensor] = None, stream=None) -> Tuple[torch.Tensor, torch.Tensor]:
         ld = _checked(logits, self._l_shape, self.dtype, self._gpu, "logits")
@@ -128,8 +132,7 @@ class RouterPlan:
                                  or bias.get_device() != self._gpu):
             raise ValueError(f"bias: expected {self.E} contiguous float32 values on the plan's GPU")
         st = self._lib.sq_route_forward(
-            logits.data_ptr(), self._type, self.T, self.E, ld, _ptr(bias), *self._rule, *self._ptrs[:4], *self._ws,
-            _on(self._gpu, stream))
+            logits.data_ptr(), *self._size, ld, _ptr(bias), *self._to, _on(self._gpu, stream))
         if st:
             _check("sq_route_forward", st)
         self._has_input = True
@@ -142,11 +145,8 @@ class RouterPlan:
         if not dshare.is_contiguous():
             raise ValueError("dshare: expected a contiguous tensor")
         ld = _checked(logits, self._l_shape, self.dtype, self._gpu, "logits")
-        score, k, _, _, renorm, scale = self._rule
-        share, chosen, _, _, dlogits = self._ptrs
         st = self._lib.sq_route_backward(
-            dshare.data_ptr(), logits.data_ptr(), self._type, self.T, self.E, ld, score, k, renorm, scale, share, chosen, dlogits,
-            self.E, _on(self._gpu, stream))
+            dshare.data_ptr(), logits.data_ptr(), *self._size, ld, *self._to_back, _on(self._gpu, stream))
         if st:
             _check("sq_route_backward", st)
         return self.dlogits
@@ -171,13 +171,18 @@ class ExchangePlan:
         self._x_shape, self._r_shape, self._k_shape = torch.Size((T, D)), torch.Size((T * k, D)), torch.Size((T, k))
         self.R = torch.zeros(self._r_shape, dtype=dtype, device=dev)
         self.out = torch.empty(self._x_shape, dtype=dtype, device=dev)
-        self._lib, self._type, self._gpu, self._ld = load(), _TYPES[dtype], _gpu_of(self.R), max(D, 1)
+        self._lib, self._gpu = load(), _gpu_of(self.R)
         self.dR = self.dX = self.dshare = None
         if train:
             self.dR, self.dX = torch.zeros_like(self.R), torch.empty_like(self.out)
             self.dshare = torch.empty((T, k), dtype=torch.float32, device=dev)
-        self._held = (self.R, self.out, self.dR, self.dX, self.dshare)      # what _ptrs point at
-        self._ptrs = tuple(map(_ptr, self._held))
+        self._held = (self.R, self.out, self.dR, self.dX, self.dshare)      # what the calls point at
+        r, out, dr, dx, dshare = ((_P, _ptr(t)) for t in self._held)
+        kind, slots = (ct.c_int32, _TYPES[dtype]), (ct.c_int32, k)
+        t, n, d, ld = (_I64, T), (_I64, T * k), (_I64, D), (_I64, max(D, 1))
+        self._x_size, self._r_size, self._slots_of = _fixed(kind, t, d), _fixed(kind, n, d), _fixed(t, slots)
+        self._to_rows, self._to_out, self._to_dx = _fixed(slots, r, n, ld), _fixed(out, ld), _fixed(dx, ld)
+        self._to_back = _fixed(dr, ld, dshare)
 
     def _slots(self, t: torch.Tensor, dtype, name: str) -> int:
         if t.dtype is not dtype or t.shape != self._k_shape or not t.is_contiguous() or t.get_device() != self._gpu:
@@ -187,18 +192,17 @@ class ExchangePlan:
     def dispatch(self, x: torch.Tensor, place: torch.Tensor, stream=None) -> torch.Tensor:
         ld = _checked(x, self._x_shape, self.dtype, self._gpu, "x")
         st = self._lib.sq_exchange_dispatch(
-            x.data_ptr(), self._type, self.T, self.D, ld, self._slots(place, torch.int32, "place"), self.k, self._ptrs[0],
-            self.rows, self._ld, _on(self._gpu, stream))
+            x.data_ptr(), *self._x_size, ld, self._slots(place, torch.int32, "place"), *self._to_rows, _on(self._gpu, stream))
         if st:
             _check("sq_exchange_dispatch", st)
         return self.R
 
-    def _combine(self, y, place, share, add, out: int, stream) -> None:
+    def _combine(self, y, place, share, add, to: tuple, stream) -> None:
         ld = _checked(y, self._r_shape, self.dtype, self._gpu, "rows")
         ld_a = 0 if add is None else _checked(add, self._x_shape, self.dtype, self._gpu, "add")
         st = self._lib.sq_exchange_combine(
-            y.data_ptr(), self._type, self.rows, self.D, ld, self._slots(place, torch.int32, "place"),
-            None if share is None else self._slots(share, torch.float32, "share"), self.T, self.k, _ptr(add), ld_a, out, self._ld,
+            y.data_ptr(), *self._r_size, ld, self._slots(place, torch.int32, "place"),
+            None if share is None else self._slots(share, torch.float32, "share"), *self._slots_of, _ptr(add), ld_a, *to,
             _on(self._gpu, stream))
         if st:
             _check("sq_exchange_combine", st)
@@ -207,7 +211,7 @@ class ExchangePlan:
                 stream=None) -> torch.Tensor:
         if share is None:
             raise ValueError("share: missing")
-        self._combine(y, place, share, add, self._ptrs[1], stream)
+        self._combine(y, place, share, add, self._to_out, stream)
         return self.out
 
     def combine_backward(self, dout: torch.Tensor, y: torch.Tensor, place: torch.Tensor, share: torch.Tensor,
@@ -218,9 +222,8 @@ class ExchangePlan:
         ld_d = _checked(dout, self._x_shape, self.dtype, self._gpu, "dout")
         ld_y = _checked(y, self._r_shape, self.dtype, self._gpu, "y")
         st = self._lib.sq_exchange_combine_backward(
-            dout.data_ptr(), y.data_ptr(), self._type, self.rows, self.D, ld_d, ld_y, self._slots(place, torch.int32, "place"),
-            self._slots(share, torch.float32, "share"), self.T, self.k, self._ptrs[2], self._ld, self._ptrs[4],
-            _on(self._gpu, stream))
+            dout.data_ptr(), y.data_ptr(), *self._r_size, ld_d, ld_y, self._slots(place, torch.int32, "place"),
+            self._slots(share, torch.float32, "share"), *self._slots_of, *self._to_back, _on(self._gpu, stream))
         if st:
             _check("sq_exchange_combine_backward", st)
         return self.dR, self.dshare
@@ -229,5 +232,5 @@ class ExchangePlan:
                           stream=None) -> torch.Tensor:
         if not self.train:
             raise ValueError("dispatch_backward needs a plan with train=True")
-        self._combine(drows, place, None, add, self._ptrs[3], stream)
+        self._combine(drows, place, None, add, self._to_dx, stream)
         return self.dX
