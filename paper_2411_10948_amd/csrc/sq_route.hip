@@ -103,19 +103,23 @@ __device__ __forceinline__ int choose(F* key, const double* s, int k, int lane, 
     return k;
 }
 
-// Leaves the groups that are not among the best top_groups out of key.  s: -inf for
-// experts that are never chosen; lds: 64 V values of the wave's own.  A group's sum is
+// How many lanes keep_groups has for a group.
+__device__ __forceinline__ int group_lanes(const RouteArgs& p) {
+    return p.groups == 1 ? 64 : 1 << (__builtin_clz((unsigned)(p.groups - 1)) - 26);      // 64 / lanes >= groups
+}
+
+// The best top_groups groups, group g at bit g group_lanes.  s: -inf for experts
+// that are never chosen; lds: 64 V values of the wave's own.  A group's sum is
 // that of its two scores plus that of their biases, so that groups which hold the
 // same of each are equal, however the biases fall on the scores.
 template <int V>
-__device__ __forceinline__ void keep_groups(const RouteArgs& p, const double* s, double* key, double* lds, int lane) {
+__device__ __forceinline__ uint64_t keep_groups(const RouteArgs& p, const double* s, double* lds, int lane) {
     const double none = -__builtin_inf();
 #pragma unroll
     for (int i = 0; i < V; ++i) lds[lane * V + i] = s[i];
     wave_fence();
     // L lanes a group, each the two highest of every L-th expert, then those of all of them
-    const int per = p.E / p.groups, shift = __builtin_clz((unsigned)max(p.groups - 1, 1)) - 26;     // 64 / L >= groups
-    const int L = p.groups == 1 ? 64 : 1 << shift, g = lane / L, first = lane % L;
+    const int per = p.E / p.groups, L = group_lanes(p), g = lane / L, first = lane % L;
     double a = none, b = none;
     int at_a = 0, at_b = 0;
     auto take = [&](double v, int at) {
@@ -150,13 +154,9 @@ __device__ __forceinline__ void keep_groups(const RouteArgs& p, const double* s,
         const double t = lds[o];
         rank += t > total || (t == total && o < g) ? 1 : 0;
     }
-    const uint64_t kept = __ballot(first == 0 && g < p.groups && rank < p.top_groups);      // of group g at bit g L
+    const uint64_t kept = __ballot(first == 0 && g < p.groups && rank < p.top_groups);
     wave_fence();
-#pragma unroll
-    for (int i = 0; i < V; ++i) {
-        const int e = lane * V + i, at = min(e / per, p.groups - 1);
-        key[i] = kept >> (at * L) & 1 ? key[i] : none;
-    }
+    return kept;
 }
 
 // The shares of a token's slots from their scores, a lane each.
@@ -196,7 +196,13 @@ __device__ __forceinline__ void wave_token(const RouteArgs& p, int64_t t, int bi
             }
             nan = __ballot(bad) != 0;
             if (!nan) {
-                if (p.groups > 1) keep_groups<V>(p, of, key, lds, lane);
+                if (p.groups > 1) {
+                    const uint64_t kept = keep_groups<V>(p, of, lds, lane);
+                    const int per = p.E / p.groups, L = group_lanes(p);
+#pragma unroll
+                    for (int k = 0; k < V; ++k)
+                        key[k] = kept >> (min((lane * V + k) / per, p.groups - 1) * L) & 1 ? key[k] : none;
+                }
                 choose<V>(key, s, p.k, lane, chosen, score);
             }
         } else {
@@ -391,12 +397,29 @@ __global__ __launch_bounds__(1024) void k_route_lanes(RouteArgs p, int lanes, in
                 const float other = __shfl(total, (lane & 48) + o * lanes);
                 rank += other > total || (other == total && o < g) ? 1 : 0;
             }
-            const bool mine = g < p.groups, kept = mine && rank < p.top_groups;
+            const bool mine = g < p.groups;
+            bool kept = mine && rank < p.top_groups;
             const float low = -max16(kept ? -total : none), high = max16(mine && !kept ? total : none);
             // Of equal totals the lowest group, but only fp64 knows which are equal: two sums with a bias and their total
             // are rounded, 3 2^-24 of the summands' size, on either side.
             const float size = max16(mine && a > none ? fabsf(a) + (b > none ? fabsf(b) : 0.0f) : 0.0f);
-            if (high > none && !(low - high > 2.0f * doubt + 0x1p-21f * size)) bad = true;
+            const bool unclear = high > none && !(low - high > 2.0f * doubt + 0x1p-21f * size);
+            // These tokens' groups by the whole wave in fp64: 16384 tokens, 4 of 8 groups of 256 experts, where one or two are
+            // unclear 28.5 -> 23 us.  With 32 experts a lane that spills, and every launch pays (34 -> 39.5 us, 2 of 4 groups of
+            // 512 experts): there the whole token is done again.
+            if constexpr (R > 16) bad |= unclear;
+            else for (uint64_t todo = __ballot(live && unclear && sub == 0); todo; todo &= todo - 1) {
+                constexpr int V = kLaneExperts / 64;
+                const int from = __ffsll((unsigned long long)todo) - 1;
+                float v[V];
+                double of[V];
+                load_logits<T, V>(static_cast<const T*>(p.logits) + (t0 + wave * 4 + (from >> 4)) * p.ld, p.E, lane, v);
+                scores<V>(v, softmax, of);
+#pragma unroll
+                for (int r = 0; r < V; ++r) of[r] = v[r] > none ? of[r] : -__builtin_inf();
+                const uint64_t best = keep_groups<V>(p, of, lds[wave], lane);
+                if ((lane ^ from) < 16) kept = mine && (best >> (g * group_lanes(p)) & 1);
+            }
 #pragma unroll
             for (int r = 0; r < R; ++r) key[r] = kept ? key[r] : 0u;
         }
