@@ -80,6 +80,18 @@ def test_quantize_both_axes(f8, M, C, square, dtype):
     np.testing.assert_array_equal(_np(a.values(_dtype("bf16"))), ref.f8_values(v, square))
 
 
+# more than 128 and 256 tiles of 128 x 128: one block for both axes
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("square", [False, True])
+@pytest.mark.parametrize("M,C", [(1500, 1540), (2060, 2100)])
+def test_quantize_both_axes_of_many_tiles(f8, M, C, square, dtype):
+    x = _rand(np.random.default_rng(M), (M, C), dtype, 3.0)
+    v = _np(x)
+    a, t = f8.quantize(x, square, True, True)
+    _check_matrix(a, ref.f8_codes(v, square), M, C)
+    _check_matrix(t, ref.f8_codes(v.T, square), C, M)
+
+
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 def test_padding_of_the_last_tile_is_zero(f8, dtype):
     # K up to a multiple of 128 is multiplied
