@@ -118,6 +118,22 @@ def test_sums_that_fp32_cannot_tell_apart(route, score, groups, k):
     _check(route, _cuda(step), k, score, 0.1 * rng.standard_normal(96), groups, max(1, groups - 1))
 
 
+@pytest.mark.parametrize("E,groups,top_groups", [(64, 16, 5), (256, 8, 4), (512, 4, 2), (1000, 10, 7)])
+@pytest.mark.parametrize("score", ["softmax", "sigmoid"])
+def test_groups_that_fp32_cannot_tell_apart(route, score, E, groups, top_groups):
+    # the same logits in every group, each in an order of its own, the highest up to two ulp apart; some tokens with NaN
+    rng = np.random.default_rng(E)
+    per = E // groups
+    v = np.sort(rng.standard_normal((130, 1, per)).astype(np.float32), 2).repeat(groups, 1)
+    for _ in range(2):
+        up = rng.random((130, groups)) < 0.4
+        v[:, :, -1] = np.where(up, np.nextafter(v[:, :, -1], np.float32(9)), v[:, :, -1])
+    logits = rng.permuted(v, axis=2).reshape(130, E)
+    logits[::9, 3] = np.nan
+    for bias in (None, np.full(E, 0.25)):
+        _check(route, _cuda(logits), 6, score, bias, groups, top_groups, renorm=True)
+
+
 @pytest.mark.parametrize("E,k", [(1, 1), (5, 5), (64, 64), (65, 64), (1024, 64)])
 def test_every_expert_chosen(route, E, k):
     _check(route, _cuda(np.random.default_rng(E).standard_normal((70, E))), k, renorm=True)
