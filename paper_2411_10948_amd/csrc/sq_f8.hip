@@ -260,10 +260,10 @@ hipError_t quantize(const F8QuantArgs& a, hipStream_t s) {
         else k_f8_quantize<T, false, apart><<<blocks, threads, 0, s>>>(a, (uint32_t)tiles_c, (uint32_t)tiles);
         return hipGetLastError();
     };
-    // Few tiles: the chip has room for a block an axis, which takes half of the steps; the second read comes from the caches.
-    // 768 x 768 (36 tiles) 4.2 us together and 3.6 apart in fp32, 4.6 and 3.7 in bf16; 2048 x 2048 (256) 5.4 and 5.2, 5.8 and
-    // 5.1; square, fp32, 3152 x 768 (150) 4.8 and 5.0; 4096 x 2048 (512) 9.2 and 12.6, 8.4 and 7.9.
-    return a.codes && a.codes_t && tiles <= (a.square && sizeof(T) == 4 ? 128 : 256) ? launch(std::true_type()) : launch(std::false_type());
+    // Few tiles: the chip has room for a block an axis, which takes half of the steps, where the second read does not count.
+    // Inputs from HBM, in fp32 768 x 768 (36 tiles) 5.1 us together and 4.3 apart, 2048 x 1024 (128) 6.0 and 5.4, 3152 x 768
+    // (150) 6.1 and 6.7; in bf16 5.1 and 4.0, 5.7 and 4.7, 5.9 and 5.6, 2048 x 2048 (256) 6.8 and 6.2.
+    return a.codes && a.codes_t && tiles <= (sizeof(T) == 4 ? 128 : 256) ? launch(std::true_type()) : launch(std::false_type());
 }
 
 }  // namespace
