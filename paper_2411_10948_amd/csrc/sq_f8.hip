@@ -4,7 +4,7 @@
 // (f8_scale), codes x 2^(127 - s) rounded to E4M3.  Every step is exact but the
 // rounding itself: the scale is a power of two taken from the exponent of the
 // maximum.  One read for both axes, bound by HBM: 8192 x 11008 in bf16 to codes along
-// both 62 us, 5.8 TB/s; 3152 x 768 in fp32 4.8 us, where the launch and the two
+// both 62 us, 5.8 TB/s; 3152 x 768 in fp32 6.1 us, where the launch and the two
 // dependent passes count.
 #include <algorithm>
 #include <type_traits>
