@@ -511,7 +511,8 @@ __global__ __launch_bounds__(1024) void k_route_lanes(RouteArgs p, int lanes, in
                 if (sub >= found) chosen = -1, s = 0.0, v = -__builtin_inf();
             }
             const double edge = __shfl(v, (lane & 48) + p.k - 1);
-            unsure = last > none && !(edge - (double)last > (double)(doubt + 0x1p-17f * fabsf(last)));
+            // a last candidate of +inf is NaN here, by the register in its last bits: in doubt too
+            unsure = last != none && !(edge - (double)last > (double)(doubt + 0x1p-17f * fabsf(last)));
         }
         if (sub >= p.k) chosen = -1, s = 0.0;
     }
