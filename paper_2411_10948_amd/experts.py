@@ -90,7 +90,8 @@ class ExpertBlock:
     """h = x + residual, y = norm(h), out = shared MLP(y) + sum over the chosen experts of share MLP_e(y),
     for ``tokens`` rows of ``dim``: ``experts`` gated MLPs of ``hidden`` units in microscaled 4 bits, ``top_k``
     of them a token, and one of ``shared`` units in 8 bits (0: none).  The router takes y in float32; its
-    rule (``score``, ``groups``, ``top_groups``, ``renormalize``, ``scale``) is ``RouterPlan``'s.
+    rule (``score``, ``groups``, ``top_groups``, ``renormalize``, ``scale``) is ``RouterPlan``'s.  A token whose
+    shares are NaN (NaN among its logits, +Inf under softmax) has NaN in all of its out.
 
     Training (``train=True``): ``set_weights``, ``forward``, ``backward``; serving: ``set_weights`` once, ``forward``
     for any inputs of ``tokens`` rows.  Results are the layer's buffers, overwritten by its next call; no step
@@ -113,6 +114,7 @@ class ExpertBlock:
             self.shared_up = f8.LinearPlan(tokens, dim, 2 * shared, train=train, **kw)
             self.shared_act = mx.ActPlan(tokens, shared, "silu", gated=True, **kw)
             self.shared_down = f8.LinearPlan(tokens, shared, dim, train=train, **kw)
+        self._zero = torch.zeros(1, device=device)
         self._codes: tuple = (None, None, None, None)
         self._weights: Optional[tuple] = None
         self._saved: Optional[tuple] = None
@@ -154,7 +156,8 @@ class ExpertBlock:
             dense = self.shared_down.forward(self.shared_act.forward(self.shared_up.forward(y, s1)), s2)
         if self.train:
             self._saved = y, logits, share, place, z
-        return self.exchange.combine(z, place, share, dense), self.norm.H
+        # such a token has no rows to bring its NaN back: share 0 adds it, and nothing to the others
+        return self.exchange.combine(z, place, share, dense).addcmul_(share[:, :1], self._zero), self.norm.H
 
     def backward(self, dout: torch.Tensor, dh: Optional[torch.Tensor] = None) -> Dict[str, torch.Tensor]:
         """Gradients of the last forward, dh that of h: x (the residual's too), gamma, beta, router, w1, w2 and, with a shared
