@@ -882,8 +882,9 @@ sq_status sq_act_backward(const void* dH, int32_t type, int32_t kind, int32_t ga
  * h (X without a residual) and the forward's stats [M, 4] (fp32, 16-byte aligned;
  * the forward takes NULL where there is no backward); dH, the gradient that
  * reaches h past the norm, may be NULL; dX is the gradient of x and of the
- * residual.  M = 0 gives dgamma = dbeta = 0.  A row that holds NaN or Inf gives
- * NaN in all of its y and dx, and in all of dgamma.  H may be X or residual, dX
+ * residual.  M = 0 gives dgamma = dbeta = 0.  A row that holds NaN or Inf, or whose
+ * sum of h passes fp32's range, gives NaN in all of its y and dx, and in all of
+ * dgamma; squares that pass it, or vanish below it, do no harm.  H may be X or residual, dX
  * may be dH, in place; no other buffers overlap.  M < 2^31, C < 2^20.
  * Workspace: sq_norm_backward_workspace_size bytes, 16-byte aligned.
  * Errors: SQ_ERR_INVALID_ARGUMENT, SQ_ERR_WORKSPACE_TOO_SMALL, SQ_ERR_HIP.

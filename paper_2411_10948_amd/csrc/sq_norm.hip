@@ -10,7 +10,8 @@
 // 6.0, 8.3 and 4.0, one row of 4096 3.5, which are launches and chains of loads and sums.
 // The mean is a sum of two fp32 numbers: the rounded mean, and the mean of what
 // is left once that is taken off, so that a row far from zero loses no digits
-// (var = mean (h - mean)^2 - rest^2).
+// (var = mean (h - mean)^2 - rest^2).  Where the squares leave fp32's range they are
+// summed up once more of deviations times a power of two (square_scale).
 #include <algorithm>
 
 #include "sq_block.h"
@@ -78,9 +79,24 @@ __device__ __forceinline__ void load_param(const void* p, int type, int C, float
     for (int v = 0; v < V; ++v) load_values<kVec<T>, WHOLE>(p, type, (v * TPR + (int)threadIdx.x % TPR) * kVec<T>, C, f + v * kVec<T>);
 }
 
+// Power of two for the deviations of a row whose sum of squares is `sum`, 1 where they are
+// fine as they are.  Inf: of up to 2^20 deviations below 2^128 one is past 2^53.  Tiny ones,
+// which count where eps does not: all are below 2^-45.
+__device__ __forceinline__ float square_scale(float sum, float eps) {
+    return sum == __builtin_inff() ? 0x1p-96f : sum < 0x1p-90f && eps < 0x1p-100f ? 0x1p96f : 1.0f;
+}
+// 1 / sqrt(var + eps) of a row from its sums of deviations times `up`, their plain sum (then
+// their mean, without `up`) and that of their squares.  A NaN in the row is one in the
+// squares, which fmaxf would drop.
+__device__ __forceinline__ float row_rstd(float* t, float inv, float eps, float up) {
+    const float rest = t[0] * inv, var = fmaxf(__builtin_fmaf(-rest, rest, t[1] * inv), 0.0f);
+    t[0] = up == 1.0f ? rest : up < 1.0f ? rest * 0x1p96f : rest * 0x1p-96f;
+    return t[1] != t[1] ? t[1] : up / sqrtf(var + eps * up * up);
+}
+
 // TPR threads a row, V pieces of 16 bytes a thread; THREADS / TPR rows at a time.
 template <typename T, int TPR, int V, int THREADS, bool WHOLE, bool NT>
-__global__ __launch_bounds__(THREADS) void k_norm_forward(NormArgs p) {
+__global__ __launch_bounds__(THREADS, WHOLE ? 4 : 2) void k_norm_forward(NormArgs p) {
     constexpr int N = kVec<T>, ROWS = THREADS / TPR;
     __shared__ float red1[ROWS][TPR / 64][1], red2[ROWS][TPR / 64][2];
     const int grp = __builtin_amdgcn_readfirstlane(threadIdx.x / TPR), tid = threadIdx.x % TPR, C = (int)p.C;
@@ -93,8 +109,8 @@ __global__ __launch_bounds__(THREADS) void k_norm_forward(NormArgs p) {
         const bool live = row < p.M;
         const T* x = static_cast<const T*>(p.x) + row * p.ld_x;
         const T* res = static_cast<const T*>(p.residual) + row * p.ld_r;
-        uint32_t w[V][4], r[V][4];
-        float f[V * N];
+        uint32_t w[V][4], r[V][4];      // h as it is stored, unpacked for each step: fewer registers than its values
+        float f[N];
 #pragma unroll
         for (int v = 0; v < V; ++v) {
             const int c = (v * TPR + tid) * N;
@@ -108,37 +124,45 @@ __global__ __launch_bounds__(THREADS) void k_norm_forward(NormArgs p) {
 #pragma unroll
         for (int v = 0; v < V; ++v) {
             const int c = (v * TPR + tid) * N;
-            values16<T>(w[v], f + v * N);
+            values16<T>(w[v], f);
             if (p.residual) {
                 float a[N];
                 values16<T>(r[v], a);
 #pragma unroll
-                for (int e = 0; e < N; ++e) a[e] += f[v * N + e];
+                for (int e = 0; e < N; ++e) a[e] += f[e];
                 pack16<T>(a, w[v]);
-                values16<T>(w[v], f + v * N);
+                values16<T>(w[v], f);
                 if (live && c < C) store16<WHOLE, NT>(static_cast<T*>(p.h) + row * p.ld_h, c, C, w[v]);
             }
 #pragma unroll
-            for (int e = 0; e < N; ++e) s[0] += f[v * N + e];
+            for (int e = 0; e < N; ++e) s[0] += f[e];
         }
         row_sum<TPR, 1>(s, red1[grp]);
         const float mean = s[0] * inv;
-        float t[2] = {0.0f, 0.0f};
+        float t[2];
+        auto squares = [&](float up) {
+            t[0] = t[1] = 0.0f;
 #pragma unroll
-        for (int v = 0; v < V; ++v) {
-            const int c = (v * TPR + tid) * N;
+            for (int v = 0; v < V; ++v) {
+                const int c = (v * TPR + tid) * N;
+                values16<T>(w[v], f);
 #pragma unroll
-            for (int e = 0; e < N; ++e) {
-                const float d = (WHOLE ? c : c + e) < C ? f[v * N + e] - mean : 0.0f;
-                f[v * N + e] = d;
-                t[0] += d;
-                t[1] = __builtin_fmaf(d, d, t[1]);
+                for (int e = 0; e < N; ++e) {
+                    const float d = (WHOLE ? c : c + e) < C ? (f[e] - mean) * up : 0.0f;
+                    t[0] += d;
+                    t[1] = __builtin_fmaf(d, d, t[1]);
+                }
             }
-        }
+        };
+        squares(1.0f);
         row_sum<TPR, 2>(t, red2[grp]);
-        const float rest = t[0] * inv, var = fmaxf(__builtin_fmaf(-rest, rest, t[1] * inv), 0.0f);
-        // a NaN in the row is one in var, which fmaxf would drop
-        const float rstd = t[1] != t[1] ? t[1] : 1.0f / sqrtf(var + p.eps);
+        const float up = square_scale(t[1], p.eps);
+        if (up != 1.0f) {       // of the whole row, which is the block's only one where it takes more than a wave
+            squares(up);
+            if constexpr (TPR > 64) __syncthreads();
+            row_sum<TPR, 2>(t, red2[grp]);
+        }
+        const float rstd = row_rstd(t, inv, p.eps, up), rest = t[0];
         if (!live) continue;
         if (p.stats && tid == 0) *reinterpret_cast<float4*>(p.stats + row * 4) = make_float4(mean, rest, rstd, 0.0f);
         T* y = static_cast<T*>(p.y) + row * p.ld_y;
@@ -146,10 +170,10 @@ __global__ __launch_bounds__(THREADS) void k_norm_forward(NormArgs p) {
         for (int v = 0; v < V; ++v) {
             const int c = (v * TPR + tid) * N;
             if (c >= C) continue;
-            float o[N];
+            values16<T>(w[v], f);
 #pragma unroll
-            for (int e = 0; e < N; ++e) o[e] = __builtin_fmaf((f[v * N + e] - rest) * rstd, g[v * N + e], b[v * N + e]);
-            pack16<T>(o, w[v]);
+            for (int e = 0; e < N; ++e) f[e] = __builtin_fmaf(((f[e] - mean) - rest) * rstd, g[v * N + e], b[v * N + e]);
+            pack16<T>(f, w[v]);
             store16<WHOLE, NT>(y, c, C, w[v]);
         }
     }
@@ -315,7 +339,7 @@ __global__ __launch_bounds__(kLong) void k_norm_forward_long(NormArgs p) {
     const float inv = 1.0f / (float)p.C;
     for (int64_t row = blockIdx.x; row < p.M; row += gridDim.x) {
         const T* x = static_cast<const T*>(p.x) + row * p.ld_x;
-        float s[1] = {0.0f}, t[2] = {0.0f, 0.0f};
+        float s[1] = {0.0f}, t[2];
         pieces<T>(p.C, [&](int c) {
             uint32_t w[4], r[4];
             float f[N], a[N];
@@ -336,21 +360,30 @@ __global__ __launch_bounds__(kLong) void k_norm_forward_long(NormArgs p) {
         if (p.residual) x = static_cast<const T*>(p.h) + row * p.ld_h;      // a thread's own stores
         row_sum<kLong, 1>(s, red1);
         const float mean = s[0] * inv;
-        pieces<T>(p.C, [&](int c) {
-            uint32_t w[4];
-            float f[N];
-            load16(x, c, p.C, w);
-            values16<T>(w, f);
+        auto squares = [&](float up) {
+            t[0] = t[1] = 0.0f;
+            pieces<T>(p.C, [&](int c) {
+                uint32_t w[4];
+                float f[N];
+                load16(x, c, p.C, w);
+                values16<T>(w, f);
 #pragma unroll
-            for (int e = 0; e < N; ++e) {
-                const float d = c + e < p.C ? f[e] - mean : 0.0f;
-                t[0] += d;
-                t[1] = __builtin_fmaf(d, d, t[1]);
-            }
-        });
+                for (int e = 0; e < N; ++e) {
+                    const float d = c + e < p.C ? (f[e] - mean) * up : 0.0f;
+                    t[0] += d;
+                    t[1] = __builtin_fmaf(d, d, t[1]);
+                }
+            });
+        };
+        squares(1.0f);
         row_sum<kLong, 2>(t, red2);
-        const float rest = t[0] * inv, var = fmaxf(__builtin_fmaf(-rest, rest, t[1] * inv), 0.0f);
-        const float rstd = t[1] != t[1] ? t[1] : 1.0f / sqrtf(var + p.eps);
+        const float up = square_scale(t[1], p.eps);
+        if (up != 1.0f) {
+            __syncthreads();
+            squares(up);
+            row_sum<kLong, 2>(t, red2);
+        }
+        const float rstd = row_rstd(t, inv, p.eps, up), rest = t[0];
         if (p.stats && threadIdx.x == 0) *reinterpret_cast<float4*>(p.stats + row * 4) = make_float4(mean, rest, rstd, 0.0f);
         pieces<T>(p.C, [&](int c) {
             uint32_t w[4];
