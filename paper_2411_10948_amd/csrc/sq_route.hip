@@ -771,18 +771,21 @@ hipError_t choices(const RouteArgs& a, int64_t blocks, hipStream_t s) {
     });
 }
 
-// Bytes of counts that all blocks together read to place their rows without a launch
-// that sums them up first.  Forward of 16384 tokens, 4 of 64 experts (4 MB) 9.5 us, with
-// the launch 15.8; of 65536 (64 MB) 27.5 and 42.2; 4 of 256 experts, 32768 tokens (64 MB)
-// 27.8 and 34.7, 65536 (256 MB) 67.4 and 61.7.
-constexpr int64_t kCounted = 128 << 20;
+// All blocks' counts are read by every block, to place its rows without a launch that
+// sums them up first, up to these bytes in all and these blocks (a 16th of them a
+// thread, one after the other: few experts are few bytes and as long).  With and without that
+// launch: 16384 tokens, 4 of 64 experts (4 MB) 15.8 and 9.9 us; 65536 (64 MB) 43 and 28; 4 of 256,
+// 32768 tokens (64 MB) 34.7 and 27.8, 65536 (256 MB) 61.7 and 67.4.  One of 4 experts: 65536
+// tokens (1024 blocks) 30 and 25, 131072 (2048) 52 and 57, 262144 102 and 168, 370000 154 and 311;
+// two of 8: 131072 63 and 51, 262144 117 and 161.
+constexpr int64_t kCounted = 128 << 20, kCountedBlocks = 2048;
 
 template <typename T>
 hipError_t forward(const RouteArgs& a, hipStream_t s) {
     const int64_t blocks = route_blocks(a.T);
     hipError_t e = a.bias || a.groups > 1 ? choices<T, true>(a, blocks, s) : choices<T, false>(a, blocks, s);
     if (e != hipSuccess || blocks == 1) return e;
-    if (blocks * blocks * a.E <= kCounted) {
+    if (blocks <= kCountedBlocks && blocks * blocks * route_stride(a.E) <= kCounted) {
         k_route_place<true><<<(uint32_t)blocks, 1024, 0, s>>>(a, (int)blocks);
         return hipGetLastError();
     }
