@@ -921,7 +921,8 @@ sq_status sq_norm_backward(const void* dY, const void* H, const void* dH, int32_
  *
  * sq_route_backward -- the logits' gradient from dshare [T, k], the forward's
  * logits, share and chosen (the choice has no gradient); slots with chosen = -1
- * count for nothing, a token whose shares are NaN gets NaN.  Every element of
+ * count for nothing, a token whose shares are NaN gets NaN.  A sigmoid's 1 - s is
+ * formed in 64 bits from s, off by 2^-53 at most.  Every element of
  * dlogits [T, E] is written; it may be the logits, in place.
  * Errors: SQ_ERR_INVALID_ARGUMENT, SQ_ERR_UNSUPPORTED, SQ_ERR_WORKSPACE_TOO_SMALL,
  * SQ_ERR_HIP.

@@ -11,12 +11,15 @@
 // drops what lies more than 13 bits below (measured: 2^16 - 2^16 + p keeps p down to
 // 2^3).  Sums of 4096 products of normal values are off by 1.5e-5 of their size so,
 // 6.5e-5 where channels differ in size: nothing next to the 2^-9 of a result in
-// bf16, but too much for one in fp32.  Those (EXACT) take the codes' values in bf16,
+// bf16 (1024 x 4096 x 2048 is 1.6548e-3 off 64 bits, rounded once from 64 bits 1.6547e-3; 1.5 % of
+// the values take their other neighbour), but too much for one in fp32.  Those (EXACT) take the codes' values in bf16,
 // which holds code and scale together, and v_mfma_f32_32x32x16_bf16, whose sums keep
 // 24 bits: 1e-8 to 1e-7, at 1.8 instead of 4.0 PFLOP/s (register loops on random codes).
-// Bound by the power that the matrix instructions take: 4096 x 11008 x 8192 runs at 2.5
-// PFLOP/s with bf16 results and at 1.37 with fp32 (a bf16 library product of 8192^3 at
-// 1.25), small ones by the launch and the first loads.
+// Large ones are bound by the matrix instructions, at what power leaves of the clock and
+// where the waves keep these fed: 8192 x 11008 x 4096 with bf16 results (300 us, 2.5 PFLOP/s) has
+// them busy for 73 % of the cycles at 1.9 GHz, on zeros for 72 % at 2.4 (218 us); with fp32
+// results for 79 % at 1.8 and 78 % at 2.4 GHz (534 and 395 us).  A bf16 library product of 8192^3 runs
+// at 1.25 PFLOP/s.  Small ones are bound by the launch and the first loads.
 #include <algorithm>
 #include <type_traits>
 
@@ -706,7 +709,7 @@ hipError_t launch_f8_gemm_pair(const F8GemmArgs& a, const F8GemmArgs& b, hipStre
 }
 
 // Few rows, for which the products' tiles would be mostly empty.  bf16, and the quantizer
-// with the product: 64 x 4096 -> 4096 (38912 of the 40000) 9.2 us, 13.5; 96 rows of it
+// with the product, one W over and over: 64 x 4096 -> 4096 (38912 of the 40000) 9.3 us, 13.5; 96 rows of it
 // (58368) 14.4, 14.0; 512 x 1024 -> 1024 (28672) 6.1, 8.7; fp32: 512 x 768 -> 768
 // (36864) 7.1, 9.5, 32 x 4096 -> 4096 (38912) 11.3, 15.5.
 bool f8_rows_ok(int64_t M, int64_t K, int64_t N, int type) {
@@ -719,7 +722,7 @@ hipError_t launch_f8_rows(const F8RowsArgs& a, hipStream_t s) {
     // One tile of rows: as many blocks as there are (1 x 4096 -> 11008 in bf16 11.6 us, with 32 columns a block 12.3), fp32
     // rows with twice the waves where these have two tiles each (1 x 4096 -> 4096 6.8 us, 7.9 with eight).  More rows:
     // columns that share the rows' codes (64 x 4096 -> 4096 10.5 us with 64 columns a block, 12.8 with 32, 19.6 with 16;
-    // 128 x 1024 -> 1024, 512 tiles, 3.9 with 32 and 4.2 with 64).
+    // 128 x 1024 -> 1024, 512 tiles, 3.9 with 32 and 4.2 with 64).  All with 12 or more W in turn.
     const int64_t tiles_m = (a.M + 15) / 16, tiles = tiles_m * ((a.N + 15) / 16);
     if (tiles_m > 1 && tiles >= 512) {
         if (a.type == SQ_TYPE_F32) return tiles >= 1024 ? rows<float, 4, 1, 8>(a, s) : rows<float, 2, 1, 8>(a, s);

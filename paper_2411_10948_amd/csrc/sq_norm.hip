@@ -321,9 +321,11 @@ __global__ __launch_bounds__(1024) void k_norm_reduce(const float* part, int64_t
 }
 
 // ---------------------------------------------------------------------------
-// Rows too long for registers: a block of 1024 threads a row, which reads it
-// again for each step (from the caches), and the columns' sums in a kernel of
-// their own.
+// Rows too long for registers (more than 8192 elements in fp32, 16384 in bf16): a block of
+// 1024 threads a row, which reads it again for each step (from the caches), and the
+// columns' sums in a kernel of their own, which reads dy and h once more.  4000 x 12000 in
+// fp32 113 us forward (384 MB, 3.4 TB/s) and 212 backward (576 MB, 2.7), 2048 x 16384 70 and 156,
+// 2048 x 20000 in bf16 53 and 98.
 // ---------------------------------------------------------------------------
 constexpr int kLong = 1024;
 
@@ -471,9 +473,11 @@ __global__ __launch_bounds__(256) void k_norm_columns(NormArgs p) {
 }
 
 // How a row is held: threads and 16-byte pieces a thread.  A wave a row as long as its
-// registers last, for want of barriers: 3152 x 768 in fp32 (192 pieces) 5.2 us forward and
-// 10.6 backward, a block of 256 threads a row 6.5 and 10.4; 16384 x 1024 in bf16 (128) 14.0
-// and 20.3, 22.8 and 34.4; 16384 x 2048 (256) 25.1 forward, 26.9.
+// registers last, for want of barriers; a block of 256 threads a row instead, launches back to
+// back, the backward with the sums of its parts: 3152 x 768 in fp32 (192 pieces) 5.4 -> 6.7 us
+// forward, 11.1 -> 11.0 backward, in bf16 (96) 4.9 -> 6.6 and 10.6 -> 11.6; 16384 x 1024 in bf16
+// (128) 14.6 -> 24.5 and 23.2 -> 35.2, 16384 x 1536 (192) 18.9 -> 25.0 and 36.0 -> 38.0,
+// 16384 x 2048 (256) 25.1 -> 27.7 forward.
 struct RowPlan {
     int tpr, v;     // tpr 0: too long for registers
 };

@@ -11,7 +11,11 @@
 //   sigmoid                 scale d_j s_j (1 - s_j)
 //   sigmoid, renormalised   scale r_j (1 - s_j) (d_j - sum_S d_i r_i)
 // The shares and gradients of the chosen experts are computed in 64 bits, a lane
-// each: next to no time, and no ratio of scores that underflow.
+// each: next to no time, and no ratio of scores that underflow.  But for one sum: a
+// softmax that is not renormalised is divided by an fp32 sum of fp32 exponentials
+// where four tokens share a wave (up to 512 experts and 16 slots), which is off by at
+// most 20 2^-24: in 64 bits it would take an exponential for every expert.  A sigmoid's
+// 1 - s is what 64 bits leave of it, off by 2^-53 at most.
 #include <algorithm>
 
 #include "sq_block.h"
@@ -619,6 +623,8 @@ __global__ __launch_bounds__(1024) void k_route_place(RouteArgs p, int blocks) {
 
 // A wave a token.  Only softmax that is not renormalised has a gradient outside the
 // chosen experts, and reads all logits; the others read those of the chosen ones.
+// Bound by the fp64 exponentials, one for every expert: 16384 x 64 in fp32 7.5 us, 16384 x 256
+// 14.3 (34 MB, 6.5 at the copy rate), 32768 x 512 61; the renormalised ones 4.6, 7.2 and 16.4.
 template <typename T, int V>
 __global__ __launch_bounds__(256) void k_route_backward(RouteArgs p) {
     __shared__ float lds[4][64 * V];

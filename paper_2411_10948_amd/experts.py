@@ -140,7 +140,7 @@ class ExpertBlock:
             self._codes = (mx.quantize(w1)[0], mx.quantize(w2)[0], *dense)
 
     def forward(self, x: torch.Tensor, residual: torch.Tensor) -> Tuple[torch.Tensor, torch.Tensor]:
-        """(out, h) [tokens, dim]"""
+        """(out, h) [tokens, dim]; the backward pass reads h, so it is not written to before that"""
         if self._weights is None:
             raise ValueError("forward needs set_weights before it")
         gamma, beta, router, bias = self._weights
@@ -175,6 +175,8 @@ class ExpertBlock:
             da, grads["s2"] = self.shared_down.backward(dout)
             dense, grads["s1"] = self.shared_up.backward(self.shared_act.backward(da))
             dy = dy + dense.float()
+        # In bf16 the addend is rounded before the experts' part is added in fp32 and the sum is rounded once more: the exchange
+        # adds rows of its own type, and half a step of the addend is what the experts' and the shared MLP's parts are off anyway.
         dy = self.exchange.dispatch_backward(drows, place, dy.to(self.dtype))
         grads["x"], grads["gamma"], grads["beta"] = self.norm.backward(dy, self.norm.H, gamma, dh)
         grads["router"] = dlogits.t() @ y.float()
