@@ -11,10 +11,11 @@
 // drops what lies more than 13 bits below (measured: 2^16 - 2^16 + p keeps p down to
 // 2^3).  Sums of 4096 products of normal values are off by 1.5e-5 of their size so,
 // 6.5e-5 where channels differ in size: nothing next to the 2^-9 of a result in
-// bf16 (1024 x 4096 x 2048 is 1.6548e-3 off 64 bits, rounded once from 64 bits 1.6547e-3; 1.5 % of
-// the values take their other neighbour), but too much for one in fp32.  Those (EXACT) take the codes' values in bf16,
-// which holds code and scale together, and v_mfma_f32_32x32x16_bf16, whose sums keep
-// 24 bits: 1e-8 to 1e-7, at 1.8 instead of 4.0 PFLOP/s (register loops on random codes).
+// bf16 (1024 x 4096 x 2048 is 1.6548e-3 off 64 bits, where one rounding of these is
+// 1.6547e-3; 1.5 % of the values take their other neighbour), but too much for one in
+// fp32.  Those (EXACT) take the codes' values in bf16, which holds code and scale
+// together, and v_mfma_f32_32x32x16_bf16, whose sums keep 24 bits: 1e-8 to 1e-7, at
+// 1.8 instead of 4.0 PFLOP/s (register loops on random codes).
 // Large ones are bound by the matrix instructions, at what power leaves of the clock and
 // where the waves keep these fed: 8192 x 11008 x 4096 with bf16 results (300 us, 2.5 PFLOP/s) has
 // them busy for 73 % of the cycles at 1.9 GHz, on zeros for 72 % at 2.4 (218 us); with fp32
