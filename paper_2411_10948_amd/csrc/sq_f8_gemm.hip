@@ -550,6 +550,9 @@ __global__ __launch_bounds__(64 * kRowsWaves, 4) void k_f8_rows(F8RowsArgs p, ui
             for (int j = 0; j < FN; ++j) load_w(min(t + u, stop - 1), j, w[u][j], ws[u][j]);
 #pragma unroll
         for (int u = 0; u < U; ++u) {
+            // read again to keep the loads free of branches: not multiplied, or times zeros, which a value that is Inf
+            // in bf16 would make NaN
+            if (EXACT && t + u >= stop) break;
             const int at = min(t + u, stop - 1);
             uint32_t v[kWords];
             const T* from = x + at * kMxTile + (lane >> 4) * 16;
@@ -565,7 +568,7 @@ __global__ __launch_bounds__(64 * kRowsWaves, 4) void k_f8_rows(F8RowsArgs p, ui
                 }
             int sa;
             v8i a = quantize_lane<sizeof(T) == 2>(v, sa);
-            if (t + u >= stop) a = v8i{0, 0, 0, 0, 0, 0, 0, 0}, sa = 0;     // read again to keep the loads free of branches
+            if (t + u >= stop) a = v8i{0, 0, 0, 0, 0, 0, 0, 0}, sa = 0;
             const int byte = 8 * (at & 3);
 #pragma unroll
             for (int j = 0; j < FN; ++j) acc[j] = multiply(w[u][j], ws[u][j] >> byte, a, sa, acc[j]);
